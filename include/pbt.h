@@ -65,7 +65,8 @@ typedef enum {
 enum { PBT_EXPLOIT_TRUNCATION = 0, PBT_EXPLOIT_TOURNAMENT = 1, PBT_EXPLOIT_TTEST = 2 };
 enum { PBT_EXPLORE_PERTURB = 0, PBT_EXPLORE_RESAMPLE = 1 };
 enum { PBT_WL_CLASSIFIER = 1, PBT_WL_GAN = 3, PBT_WL_TRANSFORMER = 4, PBT_WL_A2C = 5 }; /* workload families */
-enum { PBT_ACT_NONE = 0, PBT_ACT_RELU = 1, PBT_ACT_GELU = 2, PBT_ACT_LEAKY_RELU = 3, PBT_ACT_TANH = 4 };
+enum { PBT_ACT_NONE = 0, PBT_ACT_RELU = 1, PBT_ACT_GELU = 2, PBT_ACT_LEAKY_RELU = 3, PBT_ACT_TANH = 4,
+       PBT_ACT_SIGMOID = 5, PBT_ACT_SILU = 6 };       /* the last two: gates of pbt_block_norm only */
 enum { PBT_OPT_SGD_MOMENTUM = 0, PBT_OPT_ADAM = 1, PBT_OPT_RMSPROP = 2 };
 enum { PBT_DTYPE_FP32 = 0, PBT_DTYPE_BF16 = 1 };      /* BF16 = bf16 operands, fp32 accumulate, fp32 master weights */
 enum { PBT_ROLE_LR = 0, PBT_ROLE_BETA1 = 1, PBT_ROLE_WD = 2, /* meaning of a hyperparameter column */
@@ -324,6 +325,110 @@ pbt_status pbt_batched_gemm_bf16(const void* d_a, int64_t lda, int64_t stride_a,
                                  int64_t ldb, int64_t stride_b, int32_t b_k_contig, void* d_c, int64_t ldc,
                                  int64_t stride_c, int32_t c_is_bf16, int32_t M, int32_t N, int32_t K, int32_t batch,
                                  void* hip_stream);
+
+/* ---- Operators around the dense products -------------------------------------------------------------
+ * What a training step does to a population's tensors besides multiplying them.  Like pbt_batched_gemm_bf16 they need
+ * no handle: all pointers named d_ are device memory of the current device, structures and arrays of them are
+ * HOST memory that is read before the call returns.  Nothing is allocated, nothing synchronises (pbt_rotary_plan
+ * included); calls can be captured into graphs.  Working memory is the caller's, and two calls that may overlap in time need
+ * two of it.  Types are PBT_DTYPE_FP32 and PBT_DTYPE_BF16; arithmetic is float or double, rounded once at the
+ * end.  Pointers are aligned to their elements; strides and pitches are in elements.  An output may lie over an input only
+ * where that is said. */
+
+/* The gradient norm of every member over all its tensors, and clipping (Pascanu et al. 2013):
+ *   norm_i = sqrt(sum over tensors and elements of g^2),   g <- g max_i / norm_i  where norm_i > max_i.
+ * h_grads[k]: [P][len] elements, members src_stride (dst_stride) apart; dst may be src (with the same stride: clipped in
+ * place), otherwise the two do not overlap and members below their bound are copied.  The largest norm of member i is read on the
+ * device, d_max_norm[i * max_norm_stride] (so a column of PBT_ARR_HYPER serves; a stride of 0: one bound for all);
+ * NULL: norms only, dst is not looked at.  d_norm (float[P], may be NULL) receives the norm before clipping.
+ * Squares are summed in double, in a fixed order: no finite gradient overflows or vanishes.  A member with a NaN has norm NaN and is not
+ * scaled; one with an infinity and no NaN has norm infinity and is multiplied by 0; a bound that is NaN does not clip, one below 0 counts as 0.
+ * n_grads >= 1, 1 <= P <= PBT_MAX_P, len >= 0.  d_work: at least what pbt_clip_work_bytes says, 8-byte aligned. */
+typedef struct {
+  const void* d_src;
+  void* d_dst;
+  int64_t len, src_stride, dst_stride;
+  int32_t dtype;
+  int32_t unused;                   /* 0 */
+} pbt_grad;
+pbt_status pbt_clip_work_bytes(const pbt_grad* h_grads, int32_t n_grads, int32_t P, size_t* bytes);
+pbt_status pbt_clip_gradients(const pbt_grad* h_grads, int32_t n_grads, int32_t P, const float* d_max_norm, int64_t max_norm_stride,
+                              float* d_norm, void* d_work, size_t work_bytes, void* hip_stream);
+
+/* Rotary positions (Su et al. 2021).  The first rot_dim elements of a head are rot_dim / 2 pairs, pair j being elements
+ * (j, j + rot_dim / 2) or (2 j, 2 j + 1); at position p it turns by the angle p f_j,
+ *   a' = gain (a cos - b sin),  b' = gain (b cos + a sin),   f_j = base^(-2 j / rot_dim);
+ * the rest of the head is copied.  For contexts longer than the trained one by `factor`:
+ *   LINEAR  f_j / factor;
+ *   BASE    base * factor^(rot_dim / (rot_dim - 2)) instead of base (the slowest pair slows by `factor`, the fastest keeps its pace);
+ *   RAMP    f_j (w + (1 - w) / factor), w = (trained_len f_j / (2 pi) - low) / (high - low) clamped to [0, 1]: pairs that turn often within
+ *           the trained length keep their pace, those that turn less than `low` times are slowed by `factor`.
+ * Angles are formed in double from 32- or 64-bit positions and reduced before they are rounded. */
+enum { PBT_ROTARY_HALF = 0, PBT_ROTARY_INTERLEAVED = 1 };
+enum { PBT_ROTARY_SCALE_NONE = 0, PBT_ROTARY_SCALE_LINEAR = 1, PBT_ROTARY_SCALE_BASE = 2, PBT_ROTARY_SCALE_RAMP = 3 };
+typedef struct {
+  int32_t rot_dim;                  /* even, 2..PBT_ROTARY_MAX_DIM */
+  int32_t layout, scaling;          /* PBT_ROTARY_*, PBT_ROTARY_SCALE_* */
+  int32_t unused;                   /* 0 */
+  double base;                      /* > 0, finite */
+  double factor;                    /* > 0, finite (LINEAR, BASE, RAMP) */
+  double trained_len, low, high;    /* RAMP: trained_len > 0, low < high */
+  double gain;                      /* finite; multiplies the rotated part */
+} pbt_rotary;
+#define PBT_ROTARY_MAX_DIM 512
+/* Writes the table of frequencies, rot_dim / 2 doubles (in turns per position), that pbt_rotary_apply reads; d_table is 8-byte aligned. */
+pbt_status pbt_rotary_plan(const pbt_rotary* r, void* d_table, size_t table_bytes, void* hip_stream);
+/* One group of heads: element (row, head, e) at d_src[row * src_row + head * src_head + e].  dst is src with the same strides (in
+ * place), or the two share no element. */
+typedef struct {
+  const void* d_src;
+  void* d_dst;
+  int64_t src_row, src_head, dst_row, dst_head;
+  int32_t heads;
+  int32_t unused;                   /* 0 */
+} pbt_heads;
+/* Turns h_groups[0 .. n_groups) (1 to 4: query and key heads of one call share their angles) of `rows` rows and `width` elements a
+ * head.  Position of row r: d_positions[r] (int32 or int64 by position_bytes 4 or 8), or with d_positions = NULL
+ * start + (period > 0 ? r % period : r).  backward = 1 applies the transposed rotation (the same gain, the angle
+ * negated): the gradient of the input from that of the output.  rows = 0 is allowed. */
+pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_heads* h_groups, int32_t n_groups, int32_t dtype, int64_t rows,
+                            int32_t width, const void* d_positions, int32_t position_bytes, int64_t start, int64_t period, int32_t backward,
+                            void* hip_stream);
+
+/* The norm after a block, its gate, the scaled residual sum and the norm before the next block:
+ *   u = N_post(y),   out = alpha x + beta a(gate) * u,   z = N_pre(out)
+ * for P members of `rows` rows of d elements (member-major: row r of member i is row i rows + r of every matrix).
+ * N_LAYER(v) = (v - mean v) / sqrt(var v + eps) * gain + bias, N_RMS(v) = v / sqrt(mean v^2 + eps) * gain + bias, N_NONE(v) = v; at most one of the two is
+ * NONE.  gate: NONE (factor 1), VECTOR (one of the parameters: a factor per channel, the same for all rows of a member) or ROWS (a matrix); a is
+ * gate_act, PBT_ACT_NONE, SIGMOID, SILU or TANH.  y, z, the gate's matrix and their gradients are of `dtype`, x, out and theirs
+ * of `res_dtype`; parameters and their gradients are float.  z is formed from out before it is rounded. */
+enum { PBT_NORM_NONE = 0, PBT_NORM_LAYER = 1, PBT_NORM_RMS = 2 };
+enum { PBT_GATE_NONE = 0, PBT_GATE_VECTOR = 1, PBT_GATE_ROWS = 2 };
+#define PBT_BLOCK_NORM_MAX_D 8192
+typedef struct {
+  int64_t rows;                     /* per member, >= 0 */
+  int32_t P, d;                     /* 1..PBT_MAX_P, 1..PBT_BLOCK_NORM_MAX_D (PBT_EUNSUPPORTED beyond) */
+  int32_t post, pre, gate, gate_act;
+  int32_t dtype, res_dtype;
+  float eps, alpha, beta;           /* eps >= 0; all finite */
+} pbt_block_norm;
+typedef struct { void* d; int64_t pitch; } pbt_rows;  /* a matrix: row n starts at d + n * pitch elements, pitch >= d */
+typedef struct {                    /* device pointers, [P][d] with `stride` elements between members; a gain that is NULL is 1, a bias 0;
+                                       in gradients: those that are NULL are not written */
+  float *post_gain, *post_bias, *pre_gain, *pre_bias, *gate;
+  int64_t stride;
+} pbt_block_params;
+/* out may lie over x, z over y (the same pitch).  z (and its fields) is ignored with pre = NONE, gate with gate != ROWS.  d_stats: float[P * rows][4] = {mean, 1 / spread} of y and of
+ * out, for the backward pass; NULL: not kept. */
+pbt_status pbt_block_norm_forward(const pbt_block_norm* n, const pbt_rows* y, const pbt_rows* x, const pbt_rows* gate, const pbt_block_params* params,
+                                  const pbt_rows* out, const pbt_rows* z, float* d_stats, void* hip_stream);
+/* Gradients of y, x, the gate's matrix and the parameters from those of out and z.  y, x, gate and d_stats are what the forward
+ * pass was given and left (out is formed again from them).  dout or dz with d = NULL: zero (not both).  dx may lie over dout, dy over dz (the same
+ * pitch).  Sums over rows have a fixed order.  d_work: at least what pbt_block_norm_work_bytes says, 16-byte aligned. */
+pbt_status pbt_block_norm_work_bytes(const pbt_block_norm* n, size_t* bytes);
+pbt_status pbt_block_norm_backward(const pbt_block_norm* n, const pbt_rows* y, const pbt_rows* x, const pbt_rows* gate, const pbt_block_params* params,
+                                   const float* d_stats, const pbt_rows* dout, const pbt_rows* dz, const pbt_rows* dy, const pbt_rows* dx,
+                                   const pbt_rows* dgate, const pbt_block_params* grads, void* d_work, size_t work_bytes, void* hip_stream);
 
 /* Kernel classes for pbt_timing_enable. */
 enum {

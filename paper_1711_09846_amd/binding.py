@@ -25,7 +25,8 @@ _ARR_DTYPE = {ARR_W32: np.float32, ARR_OPT0: np.float32, ARR_OPT1: np.float32, A
 EXPORTS = ["pbt_query_sizes", "pbt_init", "pbt_step", "pbt_eval", "pbt_exploit_explore", "pbt_get_state",
            "pbt_set_state", "pbt_state_ptr", "pbt_destroy", "pbt_last_error", "pbt_batched_gemm_bf16",
            "pbt_timing_enable", "pbt_timing_stride", "pbt_timing_read", "pbt_init_population", "pbt_set_priors",
-           "pbt_step_static", "pbt_timing_enable_classes", "pbt_timing_read_class"]
+           "pbt_step_static", "pbt_timing_enable_classes", "pbt_timing_read_class", "pbt_clip_work_bytes", "pbt_clip_gradients",
+           "pbt_rotary_plan", "pbt_rotary_apply", "pbt_block_norm_forward", "pbt_block_norm_work_bytes", "pbt_block_norm_backward"]
 STATIC_SCRATCH_BYTES = 8 << 20
 (K_NONE, K_FETCH, K_GEMM_FWD, K_HEAD, K_GEMM_WGRAD, K_GEMM_DGRAD, K_BIAS_GRAD, K_OPTIMIZER, K_RANK, K_COPY,
  K_FUSED_STEP) = range(-1, 10)
@@ -55,6 +56,35 @@ class PbtLayout(C.Structure):
 
 class PbtPrior(C.Structure):
     _fields_ = [("kind", C.c_int32), ("lo", C.c_double), ("hi", C.c_double)]
+
+
+class PbtGrad(C.Structure):
+    _fields_ = [("d_src", C.c_void_p), ("d_dst", C.c_void_p), ("len", C.c_int64), ("src_stride", C.c_int64), ("dst_stride", C.c_int64),
+                ("dtype", C.c_int32), ("unused", C.c_int32)]
+
+
+class PbtRotary(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("unused", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("trained_len", C.c_double), ("low", C.c_double), ("high", C.c_double), ("gain", C.c_double)]
+
+
+class PbtHeads(C.Structure):
+    _fields_ = [("d_src", C.c_void_p), ("d_dst", C.c_void_p), ("src_row", C.c_int64), ("src_head", C.c_int64), ("dst_row", C.c_int64),
+                ("dst_head", C.c_int64), ("heads", C.c_int32), ("unused", C.c_int32)]
+
+
+class PbtBlockNorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("P", C.c_int32), ("d", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32), ("gate", C.c_int32),
+                ("gate_act", C.c_int32), ("dtype", C.c_int32), ("res_dtype", C.c_int32), ("eps", C.c_float), ("alpha", C.c_float), ("beta", C.c_float)]
+
+
+class PbtRows(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("pitch", C.c_int64)]
+
+
+class PbtBlockParams(C.Structure):
+    _fields_ = [("post_gain", C.c_void_p), ("post_bias", C.c_void_p), ("pre_gain", C.c_void_p), ("pre_bias", C.c_void_p), ("gate", C.c_void_p),
+                ("stride", C.c_int64)]
 
 
 class PbtError(RuntimeError):
@@ -94,6 +124,14 @@ def lib():
         L.pbt_timing_enable_classes.argtypes = [vp, C.c_uint32, i32]
         L.pbt_timing_read_class.argtypes = [vp, i32, C.POINTER(C.c_double), C.POINTER(i64)]
         L.pbt_timing_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(i64)]
+        L.pbt_clip_work_bytes.argtypes = [C.POINTER(PbtGrad), i32, i32, C.POINTER(sz)]
+        L.pbt_clip_gradients.argtypes = [C.POINTER(PbtGrad), i32, i32, vp, i64, vp, vp, sz, vp]
+        L.pbt_rotary_plan.argtypes = [C.POINTER(PbtRotary), vp, sz, vp]
+        L.pbt_rotary_apply.argtypes = [C.POINTER(PbtRotary), vp, C.POINTER(PbtHeads), i32, i32, i64, i32, vp, i32, i64, i64, i32, vp]
+        block, rows, params = C.POINTER(PbtBlockNorm), C.POINTER(PbtRows), C.POINTER(PbtBlockParams)
+        L.pbt_block_norm_forward.argtypes = [block, rows, rows, rows, params, rows, rows, vp, vp]
+        L.pbt_block_norm_work_bytes.argtypes = [block, C.POINTER(sz)]
+        L.pbt_block_norm_backward.argtypes = [block, rows, rows, rows, params, vp, rows, rows, rows, rows, rows, params, vp, sz, vp]
         for name in EXPORTS:
             if name != "pbt_last_error":
                 getattr(L, name).restype = C.c_int
@@ -359,3 +397,246 @@ def batched_gemm_bf16(a, b, c, M, N, K, batch, lda, sa, a_m_contig, ldb, sb, b_k
                                      C.c_void_p(torch.cuda.current_stream(a.device).cuda_stream))
     if rc != 0:
         raise PbtError(rc, lib().pbt_last_error(None).decode())
+
+
+# ---- operators around the dense products: one call each on tensors, on the current stream of the tensors' device ----------------------------
+_SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_NORMS = {"none": 0, "layer": 1, "rms": 2}
+_GATES = {"none": 0, "vector": 1, "rows": 2}
+_GATE_ACTS = {"none": 0, "tanh": 4, "sigmoid": 5, "silu": 6}
+BLOCK_PARAMS = ("post_gain", "post_bias", "pre_gain", "pre_bias", "gate")
+
+
+def _call(device, fn, *args):
+    """fn(*args, stream) with the device's current stream; kernels are launched on the current device, so it is made current if it is not."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if rc != 0:
+        raise PbtError(rc, lib().pbt_last_error(None).decode())
+
+
+def _dtype_code(t):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return 1
+    if t.dtype == torch.float32:
+        return 0
+    raise ValueError("float32 or bfloat16 tensors are wanted, not %s" % t.dtype)
+
+
+def _choice(table, value, what):
+    if value not in table:
+        raise ValueError("%s is one of %s, not %r" % (what, ", ".join(table), value))
+    return table[value]
+
+
+def _on_device(tensors, device=None):
+    for t in tensors:
+        if t.device.type != "cuda":
+            raise ValueError("device tensors are wanted")
+        if device is not None and t.device != device:
+            raise ValueError("tensors on %s and %s in one call" % (device, t.device))
+        device = t.device
+    return device
+
+
+class GradClip:
+    """Gradient norms and clipping of P members over a list of tensors (pbt_clip_gradients).
+
+    grads: tensors [P, ...], float32 or bfloat16, each member's part contiguous; outs: where the clipped gradients go (tensors of the same shapes
+    and types), None: clipped in place.  The tensors are kept, as an optimiser keeps its parameters.  A tensor may be listed once only.
+    Calling it computes the norms [P] (float32) and, with max_norm (float32 tensor [P], any stride, or of one element for all members),
+    scales every member whose norm is larger.  Without max_norm only the norms are computed."""
+
+    def __init__(self, grads, outs=None):
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if not grads or len(outs) != len(grads):
+            raise ValueError("as many outs as grads are wanted, and at least one")
+        self.device = _on_device(grads + outs)
+        self.P = grads[0].shape[0] if grads[0].dim() else 0
+        table = (PbtGrad * len(grads))()
+        for e, g, o in zip(table, grads, outs):
+            if g.dim() < 1 or g.shape[0] != self.P or o.shape != g.shape or o.dtype != g.dtype:
+                raise ValueError("tensors [P, ...] with the same P are wanted, and outs of the same shapes and types")
+            if g.numel() and not (g[0].is_contiguous() and o[0].is_contiguous()):
+                raise ValueError("a member's part of a tensor must be contiguous")
+            e.d_src, e.d_dst, e.dtype = g.data_ptr(), o.data_ptr(), _dtype_code(g)
+            e.len = g.numel() // self.P if self.P else 0
+            e.src_stride, e.dst_stride = (g.stride(0), o.stride(0)) if self.P > 1 else (e.len, e.len)
+        if len({e.d_dst for e in table if e.len}) < sum(1 for e in table if e.len):
+            raise ValueError("a tensor is listed twice")
+        self.grads, self.outs, self._table = grads, outs, table
+        n = C.c_size_t()
+        rc = lib().pbt_clip_work_bytes(table, len(grads), self.P, C.byref(n))
+        if rc != 0:
+            raise PbtError(rc, lib().pbt_last_error(None).decode())
+        self._work_bytes = n.value
+
+    def __call__(self, max_norm=None, norms=None):
+        import torch
+        if norms is None:
+            norms = torch.empty(self.P, dtype=torch.float32, device=self.device)
+        elif norms.shape != (self.P,) or norms.dtype != torch.float32 or not norms.is_contiguous() or norms.device != self.device:
+            raise ValueError("norms: a contiguous float32 tensor [P] on the gradients' device")
+        ptr = stride = 0
+        if max_norm is not None:
+            if max_norm.dtype != torch.float32 or max_norm.device != self.device or (max_norm.numel() != 1 and max_norm.shape != (self.P,)):
+                raise ValueError("max_norm: a float32 tensor [P], or of one element, on the gradients' device")
+            ptr, stride = max_norm.data_ptr(), 0 if max_norm.numel() == 1 else max_norm.stride(0)
+        work = torch.empty(self._work_bytes, dtype=torch.uint8, device=self.device)   # (of this call: calls on two streams do not meet in it)
+        _call(self.device, lib().pbt_clip_gradients, self._table, len(self.grads), self.P, ptr, stride, norms.data_ptr(), work.data_ptr(), self._work_bytes)
+        return norms
+
+
+class Rotary:
+    """Rotary positions on heads (pbt_rotary_plan, pbt_rotary_apply): rot_dim, base, layout ("half", "interleaved"), scaling ("none",
+    "linear", "base", "ramp" with factor, and for "ramp" trained, low, high) and gain as in include/pbt.h.  Making one writes the table of frequencies and
+    waits for it, so that it can be used on any stream afterwards."""
+
+    def __init__(self, rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained=0.0, low=1.0, high=32.0, gain=1.0, device="cuda:0"):
+        import torch
+        self.settings = PbtRotary(rot_dim, _choice(_LAYOUTS, layout, "layout"), _choice(_SCALINGS, scaling, "scaling"), 0, base, factor, trained, low, high, gain)
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.table = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64, device=self.device)
+        _call(self.device, lib().pbt_rotary_plan, C.byref(self.settings), self.table.data_ptr(), self.table.numel() * 8)
+        torch.cuda.current_stream(self.device).synchronize()
+
+    def __call__(self, src, dst=None, positions=None, start=0, period=0, backward=False):
+        """src: tensor [rows, heads, width] with adjacent elements, or up to four of them (query and key heads); dst: the same, None: in place.
+        positions: int32 or int64 tensor [rows]; without them row r is at start + (r % period if period else r).  backward: the transposed
+        rotation, for gradients.  Returns dst."""
+        import torch
+        if dst is None:
+            dst = src
+        many = isinstance(src, (list, tuple))
+        srcs, dsts = (src, dst) if many else ((src,), (dst,))
+        if not srcs or len(srcs) != len(dsts):
+            raise ValueError("as many dst as src are wanted, and at least one")
+        first = srcs[0]
+        groups = (PbtHeads * len(srcs))()
+        for g, a, b in zip(groups, srcs, dsts):
+            if a.dim() != 3 or b.shape != a.shape or a.shape[0] != first.shape[0] or a.shape[2] != first.shape[2]:
+                raise ValueError("src and dst: [rows, heads, width] with the same rows and width")
+            if a.dtype != first.dtype or b.dtype != first.dtype or a.device != self.device or b.device != self.device:
+                raise ValueError("src and dst: one type, on the table's device")
+            sa, sb = a.stride(), b.stride()
+            if a.shape[2] > 1 and (sa[2] != 1 or sb[2] != 1):
+                raise ValueError("a head's elements must be adjacent")
+            g.d_src, g.d_dst, g.heads = a.data_ptr(), b.data_ptr(), a.shape[1]
+            g.src_row, g.src_head, g.dst_row, g.dst_head = sa[0], sa[1], sb[0], sb[1]
+        pos, size = 0, 0
+        if positions is not None:
+            if positions.shape != (first.shape[0],) or positions.dtype not in (torch.int32, torch.int64) or not positions.is_contiguous() or positions.device != self.device:
+                raise ValueError("positions: a contiguous int32 or int64 tensor [rows] on the table's device")
+            pos, size = positions.data_ptr(), positions.element_size()
+        _call(self.device, lib().pbt_rotary_apply, C.byref(self.settings), self.table.data_ptr(), groups, len(srcs), _dtype_code(first), first.shape[0], first.shape[2],
+              pos, size, start, period, int(bool(backward)))
+        return dst
+
+
+class BlockNorm:
+    """The norm after a block, its gate, the scaled residual sum and the norm before the next block (pbt_block_norm_*), for `members`
+    networks of width `width`; post and pre: "none", "layer" or "rms"; gate: "none", "vector" or "rows"; act: "none", "sigmoid", "silu" or
+    "tanh".  params: dict with any of post_gain, post_bias, pre_gain, pre_bias and gate (the vector), float32 [members, width] (one member: [width] too), all
+    with the same distance between members."""
+
+    def __init__(self, width, members=1, post="layer", pre="layer", gate="none", act="none", eps=1e-5, alpha=1.0, beta=1.0):
+        self.width, self.members = width, members
+        self.settings = PbtBlockNorm(0, members, width, _choice(_NORMS, post, "post"), _choice(_NORMS, pre, "pre"), _choice(_GATES, gate, "gate"),
+                                     _choice(_GATE_ACTS, act, "act"), 0, 0, eps, alpha, beta)
+        self._check(lib().pbt_block_norm_work_bytes(C.byref(self.settings), C.byref(C.c_size_t())))
+
+    @staticmethod
+    def _check(rc):
+        if rc != 0:
+            raise PbtError(rc, lib().pbt_last_error(None).decode())
+
+    def _settings(self, y, x):
+        s = PbtBlockNorm.from_buffer_copy(self.settings)
+        if y.dim() != 2 or y.shape[1] != self.width or x.shape != y.shape or y.shape[0] % self.members:
+            raise ValueError("y and x: [members * rows, width]")
+        s.rows, s.dtype, s.res_dtype = y.shape[0] // self.members, _dtype_code(y), _dtype_code(x)
+        return s
+
+    @staticmethod
+    def _rows(t, like, what):
+        if t is None:
+            return PbtRows(0, 0)
+        if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+            raise ValueError("%s: shape, type and device of %s are wanted" % (what, tuple(like.shape)))
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            raise ValueError("%s: a row's elements must be adjacent" % what)
+        return PbtRows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+    def _params(self, params, device):
+        import torch
+        out, stride = PbtBlockParams(), None
+        for name, t in params.items():
+            if name not in BLOCK_PARAMS:
+                raise ValueError("unknown parameter %r" % name)
+            if t is None:
+                continue
+            if t.dtype != torch.float32 or t.device != device or t.shape[-1] != self.width or t.numel() != self.members * self.width:
+                raise ValueError("%s: float32 [members, width] on the tensors' device" % name)
+            if (self.width > 1 and t.stride(-1) != 1) or (self.members > 1 and t.dim() != 2):
+                raise ValueError("%s: float32 [members, width] with adjacent channels" % name)
+            s = t.stride(0) if self.members > 1 else self.width
+            if stride is not None and s != stride:
+                raise ValueError("parameters lie at different distances between members")
+            stride = s
+            setattr(out, name, t.data_ptr())
+        out.stride = self.width if stride is None else stride
+        return out
+
+    def forward(self, y, x, params=None, gate=None, out=None, z=None, stats=True):
+        """Returns (out, z, stats); z is None with pre = "none", stats (float32 [rows, 4], for backward) with stats = False."""
+        import torch
+        s = self._settings(y, x)
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if z is None and s.pre:
+            z = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        st = torch.empty((y.shape[0], 4), dtype=torch.float32, device=y.device) if stats else None
+        like_x = x if x.device == y.device else y
+        p = self._params(params or {}, y.device)
+        _call(_on_device((y, x)), lib().pbt_block_norm_forward, C.byref(s), C.byref(self._rows(y, y, "y")), C.byref(self._rows(x, like_x, "x")),
+              C.byref(self._rows(gate, y, "gate")), C.byref(p), C.byref(self._rows(out, x, "out")), C.byref(self._rows(z if s.pre else None, y, "z")),
+              0 if st is None else st.data_ptr())
+        return out, (z if s.pre else None), st
+
+    def backward(self, y, x, params, stats, dout, dz, gate=None, dy=None, dx=None, dgate=None, grads=None):
+        """Gradients from those of out and z (either may be None: zero).  Returns (dy, dx, dgate, grads): dgate is None unless gate = "rows";
+        grads: dict of float32 [members, width] for the parameters in params (or the tensors given as `grads`, which are overwritten)."""
+        import torch
+        s = self._settings(y, x)
+        if stats.shape != (y.shape[0], 4) or stats.dtype != torch.float32 or not stats.is_contiguous() or stats.device != y.device:
+            raise ValueError("stats: what forward returned")
+        params = params or {}
+        if dy is None:
+            dy = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        if dx is None:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        rows_gate = s.gate == 2
+        if rows_gate and dgate is None:
+            dgate = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        if grads is None:
+            names = [k for k, t in params.items() if t is not None]
+            flat = torch.empty((len(names), self.members, self.width), dtype=torch.float32, device=y.device)
+            grads = dict(zip(names, flat))
+        p, g = self._params(params, y.device), self._params(grads, y.device)
+        n = C.c_size_t()
+        self._check(lib().pbt_block_norm_work_bytes(C.byref(s), C.byref(n)))
+        work = torch.empty(n.value, dtype=torch.uint8, device=y.device)   # (of this call: calls on two streams do not meet in it)
+        _call(_on_device((y, x)), lib().pbt_block_norm_backward, C.byref(s), C.byref(self._rows(y, y, "y")), C.byref(self._rows(x, x, "x")),
+              C.byref(self._rows(gate, y, "gate")), C.byref(p), stats.data_ptr(), C.byref(self._rows(dout, x, "dout")), C.byref(self._rows(dz, y, "dz")),
+              C.byref(self._rows(dy, y, "dy")), C.byref(self._rows(dx, x, "dx")), C.byref(self._rows(dgate if rows_gate else None, y, "dgate")), C.byref(g),
+              work.data_ptr(), n.value)
+        return dy, dx, (dgate if rows_gate else None), grads

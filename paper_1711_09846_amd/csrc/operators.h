@@ -1,0 +1,98 @@
+// Launchers behind the operators of include/pbt.h that need no handle (clip.hip, rotary.hip, block_norm.hip), and what their kernels share: groups of
+// eight elements of either type at any address.  Every launcher only enqueues on `s`; arguments have been checked by the entry points.
+#pragma once
+#include <type_traits>
+
+#include "common.h"
+#include "../../include/pbt.h"
+
+namespace pbt {
+
+// ---- eight consecutive elements at an address that is a multiple of the element's size only ----
+// (global memory takes 16-byte accesses at any address: the compiler emits one for these copies, and where the address is a multiple of 16 they cost
+// what an aligned access costs)
+struct Vec16 { uint32_t w[4]; };
+__device__ __forceinline__ Vec16 load16(const void* p) { Vec16 v; __builtin_memcpy(&v, p, 16); return v; }
+__device__ __forceinline__ void store16(void* p, const Vec16& v) { __builtin_memcpy(p, &v, 16); }
+
+// elements 0 .. n-1 (n >= 8: all eight); those past n are zero
+template <class T> struct Raw8;   // eight elements as they lie in memory
+template <> struct Raw8<bf16_t> {
+  Vec16 a;
+  __device__ __forceinline__ void load(const bf16_t* p, int n) {
+    if (n >= 8) { a = load16(p); return; }
+    a = Vec16{{0, 0, 0, 0}};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (e < n) a.w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+  }
+  __device__ __forceinline__ void get(float* v) const {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) { v[2 * q] = __uint_as_float(a.w[q] << 16); v[2 * q + 1] = __uint_as_float(a.w[q] & 0xffff0000u); }
+  }
+};
+template <> struct Raw8<float> {
+  Vec16 a, b;
+  __device__ __forceinline__ void load(const float* p, int n) {
+    if (n >= 8) { a = load16(p); b = load16(p + 4); return; }
+    a = b = Vec16{{0, 0, 0, 0}};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (e < n) (e < 4 ? a : b).w[e & 3] = __float_as_uint(p[e]);
+  }
+  __device__ __forceinline__ void get(float* v) const {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) { v[q] = __uint_as_float(a.w[q]); v[4 + q] = __uint_as_float(b.w[q]); }
+  }
+};
+__device__ __forceinline__ void put8(bf16_t* p, const float* v, int n) {
+  const Vec16 o{{f2bf_pair(v[0], v[1]), f2bf_pair(v[2], v[3]), f2bf_pair(v[4], v[5]), f2bf_pair(v[6], v[7])}};
+  if (n >= 8) { store16(p, o); return; }
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) p[e] = (bf16_t)(o.w[e >> 1] >> (16 * (e & 1)));
+}
+__device__ __forceinline__ void put8(float* p, const float* v, int n) {
+  if (n >= 8) {
+    store16(p, Vec16{{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}});
+    store16(p + 4, Vec16{{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])}});
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) p[e] = v[e];
+}
+
+// ---- clip.hip ----
+size_t clip_work_bytes(const pbt_grad* g, int n, int P);
+hipError_t clip_gradients(const pbt_grad* g, int n, int P, const float* max_norm, int64_t max_norm_stride, float* norm, void* work, hipStream_t s);
+
+// ---- rotary.hip ----
+struct RotaryFrequencies { double turns[PBT_ROTARY_MAX_DIM / 2]; };
+hipError_t rotary_plan(const RotaryFrequencies& f, int n, double* table, hipStream_t s);
+struct RotaryArgs {
+  pbt_heads g[4];
+  int n_groups, heads;      // heads of all groups
+  int64_t rows;
+  int width, rot;
+  const void* pos;
+  int pos64;
+  int64_t start, period;
+  float gain, sign;         // sign of the sine: -1 transposes
+  const double* turns;
+};
+hipError_t rotary_apply(const RotaryArgs& a, int layout, int dtype, hipStream_t s);
+
+// ---- block_norm.hip ----
+struct BlockArgs {
+  pbt_block_norm n;
+  pbt_block_params p, g;    // parameters, their gradients
+  pbt_rows y, x, gate, out, z, dout, dz, dy, dx, dgate;
+  float* stats;
+  float* part;
+};
+size_t block_norm_work_bytes(const pbt_block_norm& n);
+hipError_t block_norm_forward(const BlockArgs& a, hipStream_t s);
+hipError_t block_norm_backward(const BlockArgs& a, hipStream_t s);
+
+}  // namespace pbt

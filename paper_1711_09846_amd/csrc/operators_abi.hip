@@ -1,0 +1,323 @@
+// C ABI of the operators that need no handle: arguments are checked here, on the host, before anything is launched.
+#include <cmath>
+#include <cstring>
+
+#include "handle.h"
+#include "operators.h"
+
+using namespace pbt;
+
+namespace {
+
+size_t elem_bytes(int dtype) { return dtype == PBT_DTYPE_BF16 ? 2 : 4; }
+bool known_dtype(int dtype) { return dtype == PBT_DTYPE_FP32 || dtype == PBT_DTYPE_BF16; }
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// [a, a + a_bytes) and [b, b + b_bytes) share a byte
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+
+constexpr int64_t MOST = (int64_t)1 << 46;   // lengths, strides and counts beyond it are mistakes (their products stay within 63 bits below)
+
+pbt_status check_grads(const pbt_grad* g, int n, int P, bool clip) {
+  if (!g || n < 1) return fail(nullptr, PBT_EINVAL, "no tensors are given");
+  if (P < 1 || P > PBT_MAX_P) return fail(nullptr, PBT_EINVAL, "P = %d outside 1..%d", P, PBT_MAX_P);
+  for (int k = 0; k < n; ++k) {
+    const pbt_grad& t = g[k];
+    if (!known_dtype(t.dtype)) return fail(nullptr, PBT_EINVAL, "tensor %d: unknown dtype %d", k, t.dtype);
+    if (t.unused != 0) return fail(nullptr, PBT_EINVAL, "tensor %d: the unused field must be 0", k);
+    if (t.len < 0 || t.len > MOST) return fail(nullptr, PBT_EINVAL, "tensor %d: length %lld outside 0..2^46", k, (long long)t.len);
+    if (t.len == 0) continue;
+    const size_t e = elem_bytes(t.dtype);
+    if (!t.d_src || !aligned(t.d_src, e)) return fail(nullptr, PBT_EINVAL, "tensor %d: src is NULL or not aligned to its elements", k);
+    if (P > 1 && (t.src_stride < t.len || t.src_stride > MOST)) return fail(nullptr, PBT_EINVAL, "tensor %d: src_stride below the length or above 2^46", k);
+    if (!clip) continue;
+    if (!t.d_dst || !aligned(t.d_dst, e)) return fail(nullptr, PBT_EINVAL, "tensor %d: dst is NULL or not aligned to its elements", k);
+    if (P > 1 && (t.dst_stride < t.len || t.dst_stride > MOST)) return fail(nullptr, PBT_EINVAL, "tensor %d: dst_stride below the length or above 2^46", k);
+    if (t.d_src == t.d_dst) {
+      if (P > 1 && t.src_stride != t.dst_stride) return fail(nullptr, PBT_EINVAL, "tensor %d: clipped in place with two strides", k);
+    } else {
+      const int64_t a = ((P - 1) * t.src_stride + t.len) * (int64_t)e, b = ((P - 1) * t.dst_stride + t.len) * (int64_t)e;
+      if (overlap(t.d_src, a, t.d_dst, b)) {
+        // rows of one array side by side are fine
+        const int64_t diff = static_cast<const char*>(t.d_dst) - static_cast<const char*>(t.d_src);
+        const int64_t p = t.src_stride * (int64_t)e;
+        const int64_t m = P > 1 && t.src_stride == t.dst_stride ? ((diff % p) + p) % p : 0;
+        if (m < t.len * (int64_t)e || p - m < t.len * (int64_t)e) return fail(nullptr, PBT_EINVAL, "tensor %d: src and dst overlap", k);
+      }
+    }
+  }
+  return PBT_OK;
+}
+
+pbt_status check_rotary(const pbt_rotary* r) {
+  if (!r) return fail(nullptr, PBT_EINVAL, "rotary settings are NULL");
+  if (r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > PBT_ROTARY_MAX_DIM) return fail(nullptr, PBT_EINVAL, "rot_dim = %d: even, 2..%d", r->rot_dim, PBT_ROTARY_MAX_DIM);
+  if (r->layout != PBT_ROTARY_HALF && r->layout != PBT_ROTARY_INTERLEAVED) return fail(nullptr, PBT_EINVAL, "unknown rotary layout %d", r->layout);
+  if (r->scaling < PBT_ROTARY_SCALE_NONE || r->scaling > PBT_ROTARY_SCALE_RAMP) return fail(nullptr, PBT_EINVAL, "unknown rotary scaling %d", r->scaling);
+  if (r->unused != 0) return fail(nullptr, PBT_EINVAL, "the unused field must be 0");
+  if (!(r->base > 0.0) || !std::isfinite(r->base)) return fail(nullptr, PBT_EINVAL, "base must be positive and finite");
+  if (!std::isfinite(r->gain)) return fail(nullptr, PBT_EINVAL, "gain must be finite");
+  if (r->scaling != PBT_ROTARY_SCALE_NONE && (!(r->factor > 0.0) || !std::isfinite(r->factor))) return fail(nullptr, PBT_EINVAL, "factor must be positive and finite");
+  if (r->scaling == PBT_ROTARY_SCALE_RAMP &&
+      (!(r->trained_len > 0.0) || !std::isfinite(r->trained_len) || !(r->low < r->high) || !std::isfinite(r->low) || !std::isfinite(r->high)))
+    return fail(nullptr, PBT_EINVAL, "ramp scaling needs trained_len > 0 and low < high, finite");
+  return PBT_OK;
+}
+
+// no element of one group's dst is one of its src, unless they are the same view
+bool heads_apart(const pbt_heads& g, int64_t rows, int width, int64_t e) {
+  if (g.d_src == g.d_dst && (rows == 1 || g.src_row == g.dst_row) && (g.heads == 1 || g.src_head == g.dst_head)) return true;
+  const int64_t src_row = ((g.heads - 1) * g.src_head + width) * e, dst_row = ((g.heads - 1) * g.dst_head + width) * e;   // bytes of a row's heads
+  if (!overlap(g.d_src, (rows - 1) * g.src_row * e + src_row, g.d_dst, (rows - 1) * g.dst_row * e + dst_row)) return true;
+  if (rows > 1 && g.src_row != g.dst_row) return false;
+  const int64_t p = g.src_row * e, diff = static_cast<const char*>(g.d_dst) - static_cast<const char*>(g.d_src);
+  if (rows == 1 || p <= 0) return false;
+  const int64_t m = ((diff % p) + p) % p;   // columns of one array's rows, side by side
+  return m >= src_row && p - m >= dst_row;
+}
+
+pbt_status check_block(const pbt_block_norm* n) {
+  if (!n) return fail(nullptr, PBT_EINVAL, "block norm settings are NULL");
+  if (n->P < 1 || n->P > PBT_MAX_P) return fail(nullptr, PBT_EINVAL, "P = %d outside 1..%d", n->P, PBT_MAX_P);
+  if (n->rows < 0 || n->rows > ((int64_t)1 << 40)) return fail(nullptr, PBT_EINVAL, "rows outside 0..2^40");
+  if (n->d < 1) return fail(nullptr, PBT_EINVAL, "d must be positive");
+  if (n->d > PBT_BLOCK_NORM_MAX_D) return fail(nullptr, PBT_EUNSUPPORTED, "d = %d: rows of up to %d elements are built", n->d, PBT_BLOCK_NORM_MAX_D);
+  if (n->post < PBT_NORM_NONE || n->post > PBT_NORM_RMS || n->pre < PBT_NORM_NONE || n->pre > PBT_NORM_RMS) return fail(nullptr, PBT_EINVAL, "unknown norm %d / %d", n->post, n->pre);
+  if (n->post == PBT_NORM_NONE && n->pre == PBT_NORM_NONE) return fail(nullptr, PBT_EINVAL, "neither a norm after the block nor one before the next");
+  if (n->gate < PBT_GATE_NONE || n->gate > PBT_GATE_ROWS) return fail(nullptr, PBT_EINVAL, "unknown gate %d", n->gate);
+  if (n->gate_act != PBT_ACT_NONE && n->gate_act != PBT_ACT_SIGMOID && n->gate_act != PBT_ACT_SILU && n->gate_act != PBT_ACT_TANH)
+    return fail(nullptr, PBT_EINVAL, "activation %d is none of a gate's", n->gate_act);
+  if (n->gate == PBT_GATE_NONE && n->gate_act != PBT_ACT_NONE) return fail(nullptr, PBT_EINVAL, "a gate activation without a gate");
+  if (!known_dtype(n->dtype) || !known_dtype(n->res_dtype)) return fail(nullptr, PBT_EINVAL, "unknown dtype %d / %d", n->dtype, n->res_dtype);
+  if (!(n->eps >= 0.f) || !std::isfinite(n->eps) || !std::isfinite(n->alpha) || !std::isfinite(n->beta)) return fail(nullptr, PBT_EINVAL, "eps >= 0, alpha and beta must be finite");
+  return PBT_OK;
+}
+
+// a matrix of a block norm: there (unless optional), aligned to its elements, rows that do not overlap
+pbt_status check_rows(const pbt_block_norm* n, const pbt_rows* m, const char* name, int dtype, bool optional) {
+  if (!m || !m->d) return optional ? PBT_OK : fail(nullptr, PBT_EINVAL, "%s is NULL", name);
+  if (!aligned(m->d, elem_bytes(dtype))) return fail(nullptr, PBT_EINVAL, "%s is not aligned to its elements", name);
+  if (m->pitch < n->d || m->pitch > ((int64_t)1 << 32)) return fail(nullptr, PBT_EINVAL, "%s: pitch %lld below d or above 2^32", name, (long long)m->pitch);
+  if ((int64_t)n->P * n->rows > MOST / m->pitch) return fail(nullptr, PBT_EINVAL, "%s is too large", name);
+  return PBT_OK;
+}
+pbt_status check_params(const pbt_block_norm* n, const pbt_block_params* p, const char* what) {
+  if (!p) return fail(nullptr, PBT_EINVAL, "%s are NULL", what);
+  float* const* q = &p->post_gain;
+  for (int k = 0; k < 5; ++k)
+    if (q[k] && !aligned(q[k], 4)) return fail(nullptr, PBT_EINVAL, "%s: pointer %d is not aligned to its elements", what, k);
+  if (n->P > 1 && (q[0] || q[1] || q[2] || q[3] || q[4]) && (p->stride < n->d || p->stride > MOST)) return fail(nullptr, PBT_EINVAL, "%s: stride below d or above 2^46", what);
+  return PBT_OK;
+}
+int64_t rows_bytes(const pbt_block_norm* n, const pbt_rows& m, int dtype) {
+  return n->rows == 0 ? 0 : (((int64_t)n->P * n->rows - 1) * m.pitch + n->d) * (int64_t)elem_bytes(dtype);
+}
+// an output and any other matrix of the call: apart, columns side by side in rows of one pitch, or (same_ok) the same rows
+pbt_status check_apart(const pbt_block_norm* n, const pbt_rows& out, int out_type, const char* out_name, const pbt_rows* m, int type, const char* name, bool same_ok) {
+  if (!m || !m->d || !out.d || n->rows == 0) return PBT_OK;
+  if (!overlap(out.d, rows_bytes(n, out, out_type), m->d, rows_bytes(n, *m, type))) return PBT_OK;
+  if (same_ok && out.d == m->d && out.pitch == m->pitch && out_type == type) return PBT_OK;
+  const int64_t a = (int64_t)elem_bytes(out_type), b = (int64_t)elem_bytes(type), p = out.pitch * a;
+  if (p == m->pitch * b) {
+    const int64_t diff = static_cast<const char*>(m->d) - static_cast<const char*>(out.d), at = ((diff % p) + p) % p;
+    if (at >= n->d * a && p - at >= n->d * b) return PBT_OK;
+  }
+  return fail(nullptr, PBT_EINVAL, "%s overlaps %s", out_name, name);
+}
+
+#define TRY(call) do { const pbt_status st_ = (call); if (st_ != PBT_OK) return st_; } while (0)
+
+}  // namespace
+
+extern "C" {
+
+pbt_status pbt_clip_work_bytes(const pbt_grad* h_grads, int32_t n_grads, int32_t P, size_t* bytes) {
+  if (!bytes) return fail(nullptr, PBT_EINVAL, "bytes is NULL");
+  TRY(check_grads(h_grads, n_grads, P, false));
+  *bytes = clip_work_bytes(h_grads, n_grads, P);
+  return PBT_OK;
+}
+
+pbt_status pbt_clip_gradients(const pbt_grad* h_grads, int32_t n_grads, int32_t P, const float* d_max_norm, int64_t max_norm_stride, float* d_norm, void* d_work,
+                              size_t work_bytes, void* hip_stream) {
+  TRY(check_grads(h_grads, n_grads, P, d_max_norm != nullptr));
+  if (!aligned(d_max_norm, 4) || !aligned(d_norm, 4)) return fail(nullptr, PBT_EINVAL, "max_norm and norm must be aligned to floats");
+  if (d_max_norm && (max_norm_stride < 0 || max_norm_stride > MOST)) return fail(nullptr, PBT_EINVAL, "max_norm_stride outside 0..2^46");
+  if (!d_max_norm && !d_norm) return fail(nullptr, PBT_EINVAL, "neither a bound nor a place for the norms");
+  const size_t need = clip_work_bytes(h_grads, n_grads, P);
+  if (!d_work || !aligned(d_work, 8)) return fail(nullptr, PBT_EINVAL, "work is NULL or not 8-byte aligned");
+  if (work_bytes < need) return fail(nullptr, PBT_ENOMEM, "working memory: %zu bytes given, %zu needed", work_bytes, need);
+  const hipError_t e = clip_gradients(h_grads, n_grads, P, d_max_norm, max_norm_stride, d_norm, d_work, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(nullptr, PBT_EDEVICE, "clipping failed to launch: %s", hipGetErrorString(e));
+  return PBT_OK;
+}
+
+pbt_status pbt_rotary_plan(const pbt_rotary* r, void* d_table, size_t table_bytes, void* hip_stream) {
+  TRY(check_rotary(r));
+  if (!d_table || !aligned(d_table, 8)) return fail(nullptr, PBT_EINVAL, "table is NULL or not 8-byte aligned");
+  const int pairs = r->rot_dim / 2;
+  if (table_bytes < pairs * sizeof(double)) return fail(nullptr, PBT_ENOMEM, "table: %zu bytes given, %zu needed", table_bytes, pairs * sizeof(double));
+  RotaryFrequencies f;
+  std::memset(&f, 0, sizeof f);
+  const double two_pi = 6.283185307179586476925;
+  const double base = r->scaling == PBT_ROTARY_SCALE_BASE && r->rot_dim > 2 ? r->base * std::pow(r->factor, r->rot_dim / (r->rot_dim - 2.0)) : r->base;
+  for (int j = 0; j < pairs; ++j) {
+    double w = std::pow(base, -2.0 * j / r->rot_dim);   // radians a position
+    if (r->scaling == PBT_ROTARY_SCALE_LINEAR) w /= r->factor;
+    if (r->scaling == PBT_ROTARY_SCALE_RAMP) {
+      const double at = (r->trained_len * w / two_pi - r->low) / (r->high - r->low), keep = at < 0.0 ? 0.0 : at > 1.0 ? 1.0 : at;
+      w *= keep + (1.0 - keep) / r->factor;
+    }
+    f.turns[j] = w / two_pi;
+  }
+  const hipError_t e = rotary_plan(f, pairs, static_cast<double*>(d_table), static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(nullptr, PBT_EDEVICE, "writing the rotary table failed: %s", hipGetErrorString(e));
+  return PBT_OK;
+}
+
+pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_heads* h_groups, int32_t n_groups, int32_t dtype, int64_t rows, int32_t width,
+                            const void* d_positions, int32_t position_bytes, int64_t start, int64_t period, int32_t backward, void* hip_stream) {
+  TRY(check_rotary(r));
+  if (!d_table || !aligned(d_table, 8)) return fail(nullptr, PBT_EINVAL, "table is NULL or not 8-byte aligned");
+  if (!h_groups || n_groups < 1 || n_groups > 4) return fail(nullptr, PBT_EINVAL, "1 to 4 groups of heads");
+  if (!known_dtype(dtype)) return fail(nullptr, PBT_EINVAL, "unknown dtype %d", dtype);
+  if (rows < 0 || rows > 0x7fffffffLL) return fail(nullptr, PBT_EINVAL, "rows outside 0..2^31-1");
+  if (width < r->rot_dim || width > 65536) return fail(nullptr, PBT_EINVAL, "heads of %d elements: rot_dim (%d) to 65536", width, r->rot_dim);
+  if (d_positions && position_bytes != 4 && position_bytes != 8) return fail(nullptr, PBT_EINVAL, "positions have 4 or 8 bytes");
+  if (d_positions && !aligned(d_positions, position_bytes)) return fail(nullptr, PBT_EINVAL, "positions are not aligned to their elements");
+  if (!d_positions && (period < 0 || start < -MOST || start > MOST)) return fail(nullptr, PBT_EINVAL, "period below 0, or start outside +-2^46");
+  if (backward != 0 && backward != 1) return fail(nullptr, PBT_EINVAL, "backward is 0 or 1");
+  const int64_t e = (int64_t)elem_bytes(dtype);
+  int64_t heads = 0;
+  for (int k = 0; k < n_groups; ++k) {
+    const pbt_heads& g = h_groups[k];
+    if (g.heads < 1 || g.heads > 65536) return fail(nullptr, PBT_EINVAL, "group %d: heads outside 1..65536", k);
+    if (g.unused != 0) return fail(nullptr, PBT_EINVAL, "group %d: the unused field must be 0", k);
+    heads += g.heads;
+    if (rows == 0) continue;
+    if (!g.d_src || !g.d_dst || !aligned(g.d_src, e) || !aligned(g.d_dst, e)) return fail(nullptr, PBT_EINVAL, "group %d: src or dst is NULL or not aligned to its elements", k);
+    if (g.heads > 1 && (g.src_head < width || g.dst_head < width)) return fail(nullptr, PBT_EINVAL, "group %d: heads overlap", k);
+    const int64_t limit = (int64_t)1 << 31;
+    if (g.src_row < 0 || g.dst_row < 0 || g.src_head > limit || g.dst_head > limit || g.src_row > limit || g.dst_row > limit)
+      return fail(nullptr, PBT_EINVAL, "group %d: strides above 2^31 or negative", k);
+    // dst's elements are apart: heads within rows, or rows within heads
+    const bool in_rows = g.dst_row >= (g.heads - 1) * g.dst_head + width, in_heads = g.dst_row >= width && g.dst_head >= (rows - 1) * g.dst_row + width;
+    if (rows > 1 && !(g.heads == 1 ? g.dst_row >= width : in_rows || in_heads)) return fail(nullptr, PBT_EINVAL, "group %d: rows of dst overlap", k);
+    if (!heads_apart(g, rows, width, e)) return fail(nullptr, PBT_EINVAL, "group %d: dst overlaps src and is not the same view", k);
+  }
+  if (heads > 65536) return fail(nullptr, PBT_EINVAL, "more than 65536 heads");
+  if (rows == 0) return PBT_OK;
+  RotaryArgs a;
+  std::memset(&a, 0, sizeof a);
+  for (int k = 0; k < n_groups; ++k) a.g[k] = h_groups[k];
+  a.n_groups = n_groups; a.heads = (int)heads;
+  a.rows = rows; a.width = width; a.rot = r->rot_dim;
+  a.pos = d_positions; a.pos64 = position_bytes == 8;
+  a.start = start; a.period = period;
+  a.gain = (float)r->gain; a.sign = backward ? -1.f : 1.f;
+  a.turns = static_cast<const double*>(d_table);
+  const hipError_t err = rotary_apply(a, r->layout, dtype, static_cast<hipStream_t>(hip_stream));
+  if (err != hipSuccess) return fail(nullptr, PBT_EDEVICE, "rotary positions failed to launch: %s", hipGetErrorString(err));
+  return PBT_OK;
+}
+
+pbt_status pbt_block_norm_forward(const pbt_block_norm* n, const pbt_rows* y, const pbt_rows* x, const pbt_rows* gate, const pbt_block_params* params,
+                                  const pbt_rows* out, const pbt_rows* z, float* d_stats, void* hip_stream) {
+  TRY(check_block(n));
+  const int A = n->dtype, R = n->res_dtype;
+  const bool gated = n->gate == PBT_GATE_ROWS, normed = n->pre != PBT_NORM_NONE;
+  TRY(check_params(n, params, "parameters"));
+  if (n->gate == PBT_GATE_VECTOR && !params->gate) return fail(nullptr, PBT_EINVAL, "the gate vector is NULL");
+  if (n->rows == 0) return PBT_OK;
+  TRY(check_rows(n, y, "y", A, false));
+  TRY(check_rows(n, x, "x", R, false));
+  if (gated) TRY(check_rows(n, gate, "gate", A, false));
+  TRY(check_rows(n, out, "out", R, false));
+  if (normed) TRY(check_rows(n, z, "z", A, false));
+  if (!aligned(d_stats, 16)) return fail(nullptr, PBT_EINVAL, "stats must be 16-byte aligned");
+  TRY(check_apart(n, *out, R, "out", x, R, "x", true));
+  TRY(check_apart(n, *out, R, "out", y, A, "y", false));
+  if (gated) TRY(check_apart(n, *out, R, "out", gate, A, "the gate", false));
+  if (normed) {
+    TRY(check_apart(n, *z, A, "z", y, A, "y", true));
+    TRY(check_apart(n, *z, A, "z", x, R, "x", false));
+    TRY(check_apart(n, *z, A, "z", out, R, "out", false));
+    if (gated) TRY(check_apart(n, *z, A, "z", gate, A, "the gate", false));
+  }
+  BlockArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.n = *n; a.p = *params; a.y = *y; a.x = *x; a.out = *out; a.stats = d_stats;
+  if (gated) a.gate = *gate;
+  if (normed) a.z = *z;
+  const hipError_t e = block_norm_forward(a, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(nullptr, PBT_EDEVICE, "block norm failed to launch: %s", hipGetErrorString(e));
+  return PBT_OK;
+}
+
+pbt_status pbt_block_norm_work_bytes(const pbt_block_norm* n, size_t* bytes) {
+  if (!bytes) return fail(nullptr, PBT_EINVAL, "bytes is NULL");
+  TRY(check_block(n));
+  *bytes = block_norm_work_bytes(*n);
+  return PBT_OK;
+}
+
+pbt_status pbt_block_norm_backward(const pbt_block_norm* n, const pbt_rows* y, const pbt_rows* x, const pbt_rows* gate, const pbt_block_params* params,
+                                   const float* d_stats, const pbt_rows* dout, const pbt_rows* dz, const pbt_rows* dy, const pbt_rows* dx, const pbt_rows* dgate,
+                                   const pbt_block_params* grads, void* d_work, size_t work_bytes, void* hip_stream) {
+  TRY(check_block(n));
+  const int A = n->dtype, R = n->res_dtype;
+  const bool gated = n->gate == PBT_GATE_ROWS, normed = n->pre != PBT_NORM_NONE;
+  TRY(check_params(n, params, "parameters"));
+  TRY(check_params(n, grads, "parameter gradients"));
+  if (n->gate == PBT_GATE_VECTOR && !params->gate) return fail(nullptr, PBT_EINVAL, "the gate vector is NULL");
+  if (n->gate != PBT_GATE_VECTOR && grads->gate) return fail(nullptr, PBT_EINVAL, "a gradient of the gate vector is asked for and there is none");
+  if (n->post == PBT_NORM_NONE && (grads->post_gain || grads->post_bias)) return fail(nullptr, PBT_EINVAL, "gradients of a norm after the block are asked for and there is none");
+  if (!normed && (grads->pre_gain || grads->pre_bias)) return fail(nullptr, PBT_EINVAL, "gradients of a norm before the next block are asked for and there is none");
+  const bool has_dz = normed && dz && dz->d, has_dout = dout && dout->d;
+  if (n->rows > 0) {
+    TRY(check_rows(n, y, "y", A, false));
+    TRY(check_rows(n, x, "x", R, false));
+    if (gated) TRY(check_rows(n, gate, "gate", A, false));
+    if (gated) TRY(check_rows(n, dgate, "dgate", A, false));
+    if (!has_dz && !has_dout) return fail(nullptr, PBT_EINVAL, "neither dout nor dz");
+    if (has_dz) TRY(check_rows(n, dz, "dz", A, false));
+    if (has_dout) TRY(check_rows(n, dout, "dout", R, false));
+    TRY(check_rows(n, dy, "dy", A, false));
+    TRY(check_rows(n, dx, "dx", R, false));
+    if (!d_stats || !aligned(d_stats, 16)) return fail(nullptr, PBT_EINVAL, "stats is NULL or not 16-byte aligned");
+    const struct { const pbt_rows* m; int type; const char* name; } in[5] = {{y, A, "y"}, {x, R, "x"}, {gated ? gate : nullptr, A, "the gate"},
+                                                                            {has_dz ? dz : nullptr, A, "dz"}, {has_dout ? dout : nullptr, R, "dout"}};
+    for (int k = 0; k < 5; ++k) {
+      TRY(check_apart(n, *dy, A, "dy", in[k].m, in[k].type, in[k].name, k == 3));
+      TRY(check_apart(n, *dx, R, "dx", in[k].m, in[k].type, in[k].name, k == 4));
+      if (gated) TRY(check_apart(n, *dgate, A, "dgate", in[k].m, in[k].type, in[k].name, false));
+    }
+    TRY(check_apart(n, *dy, A, "dy", dx, R, "dx", false));
+    if (gated) {
+      TRY(check_apart(n, *dgate, A, "dgate", dy, A, "dy", false));
+      TRY(check_apart(n, *dgate, A, "dgate", dx, R, "dx", false));
+    }
+    const size_t need = block_norm_work_bytes(*n);
+    if (!d_work || !aligned(d_work, 16)) return fail(nullptr, PBT_EINVAL, "work is NULL or not 16-byte aligned");
+    if (work_bytes < need) return fail(nullptr, PBT_ENOMEM, "working memory: %zu bytes given, %zu needed", work_bytes, need);
+  }
+  BlockArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.n = *n; a.p = *params; a.g = *grads;
+  a.stats = const_cast<float*>(d_stats);
+  a.part = static_cast<float*>(d_work);
+  if (n->rows > 0) {
+    a.y = *y; a.x = *x; a.dy = *dy; a.dx = *dx;
+    if (gated) { a.gate = *gate; a.dgate = *dgate; }
+    if (has_dz) a.dz = *dz;
+    if (has_dout) a.dout = *dout;
+  }
+  const hipError_t e = block_norm_backward(a, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(nullptr, PBT_EDEVICE, "block norm backward failed to launch: %s", hipGetErrorString(e));
+  return PBT_OK;
+}
+
+}  // extern "C"
