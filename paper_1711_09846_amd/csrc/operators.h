@@ -14,6 +14,13 @@ namespace pbt {
 struct Vec16 { uint32_t w[4]; };
 __device__ __forceinline__ Vec16 load16(const void* p) { Vec16 v; __builtin_memcpy(&v, p, 16); return v; }
 __device__ __forceinline__ void store16(void* p, const Vec16& v) { __builtin_memcpy(p, &v, 16); }
+// the same past the caches
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void stream16(void* p, const Vec16& v) {
+  const u32x4_any x = {v.w[0], v.w[1], v.w[2], v.w[3]};
+  __builtin_nontemporal_store(x, static_cast<u32x4_any*>(p));
+}
+constexpr int64_t LAST_CACHE = (int64_t)256 << 20;   // bytes of the cache in front of memory: what a call writes beyond it is not found there afterwards
 
 // elements 0 .. n-1 (n >= 8: all eight); those past n are zero
 template <class T> struct Raw8;   // eight elements as they lie in memory

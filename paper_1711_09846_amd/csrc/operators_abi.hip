@@ -185,7 +185,7 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
   if (!h_groups || n_groups < 1 || n_groups > 4) return fail(nullptr, PBT_EINVAL, "1 to 4 groups of heads");
   if (!known_dtype(dtype)) return fail(nullptr, PBT_EINVAL, "unknown dtype %d", dtype);
   if (rows < 0 || rows > 0x7fffffffLL) return fail(nullptr, PBT_EINVAL, "rows outside 0..2^31-1");
-  if (width < r->rot_dim || width > 65536) return fail(nullptr, PBT_EINVAL, "heads of %d elements: rot_dim (%d) to 65536", width, r->rot_dim);
+  if (width < r->rot_dim || width > 16384) return fail(nullptr, PBT_EINVAL, "heads of %d elements: rot_dim (%d) to 16384", width, r->rot_dim);
   if (d_positions && position_bytes != 4 && position_bytes != 8) return fail(nullptr, PBT_EINVAL, "positions have 4 or 8 bytes");
   if (d_positions && !aligned(d_positions, position_bytes)) return fail(nullptr, PBT_EINVAL, "positions are not aligned to their elements");
   if (!d_positions && (period < 0 || start < -MOST || start > MOST)) return fail(nullptr, PBT_EINVAL, "period below 0, or start outside +-2^46");
@@ -194,7 +194,7 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
   int64_t heads = 0;
   for (int k = 0; k < n_groups; ++k) {
     const pbt_heads& g = h_groups[k];
-    if (g.heads < 1 || g.heads > 65536) return fail(nullptr, PBT_EINVAL, "group %d: heads outside 1..65536", k);
+    if (g.heads < 1 || g.heads > 32768) return fail(nullptr, PBT_EINVAL, "group %d: heads outside 1..32768", k);
     if (g.unused != 0) return fail(nullptr, PBT_EINVAL, "group %d: the unused field must be 0", k);
     heads += g.heads;
     if (rows == 0) continue;
@@ -208,7 +208,7 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
     if (rows > 1 && !(g.heads == 1 ? g.dst_row >= width : in_rows || in_heads)) return fail(nullptr, PBT_EINVAL, "group %d: rows of dst overlap", k);
     if (!heads_apart(g, rows, width, e)) return fail(nullptr, PBT_EINVAL, "group %d: dst overlaps src and is not the same view", k);
   }
-  if (heads > 65536) return fail(nullptr, PBT_EINVAL, "more than 65536 heads");
+  if (heads > 32768) return fail(nullptr, PBT_EINVAL, "more than 32768 heads");
   if (rows == 0) return PBT_OK;
   RotaryArgs a;
   std::memset(&a, 0, sizeof a);

@@ -1,4 +1,10 @@
 // Rotary positions: pair j of a head at position p is turned by p f_j.
+//
+// Bound by memory: every element is read and written once.  The angles are what could be in the way: their sine and cosine take some sixty instructions, as
+// much as moving a pair takes at the memory's rate, so a workgroup forms them once for a few rows, in LDS, and all heads of those rows use them.  A unit of
+// work is one 16-byte access of adjacent pairs (two where a pair's halves lie apart).
+#include <algorithm>
+
 #include "operators.h"
 
 namespace pbt {
@@ -20,40 +26,214 @@ __device__ __forceinline__ float2 turn(double turns) {
   return make_float2(k == 1 || k == 2 ? -a : a, k >= 2 ? -b : b);
 }
 
-template <class T> __device__ __forceinline__ float to_float(T v);
-template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_float<bf16_t>(bf16_t v) { return bf2f(v); }
-__device__ __forceinline__ void set(float* p, float v) { *p = v; }
-__device__ __forceinline__ void set(bf16_t* p, float v) { *p = f2bf(v); }
-
 __device__ __forceinline__ int64_t position(const RotaryArgs& a, int64_t row) {
   if (a.pos) return a.pos64 ? static_cast<const int64_t*>(a.pos)[row] : (int64_t)static_cast<const int32_t*>(a.pos)[row];
   return a.start + (a.period > 0 ? row % a.period : row);
 }
 
-// one workgroup a row, one thread a pair or an element of the part that is copied
-template <class T, int LAYOUT>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
-  const int pairs = a.rot / 2, items = pairs + a.width - a.rot;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x)
-  for (int k = threadIdx.x; k < items * a.heads; k += 256) {
-    const double p = (double)position(a, row);
-    int h = k / items, j = k % items, g = 0;
-    while (h >= a.g[g].heads) h -= a.g[g++].heads;
-    const T* src = static_cast<const T*>(a.g[g].d_src) + row * a.g[g].src_row + h * a.g[g].src_head;
-    T* dst = static_cast<T*>(a.g[g].d_dst) + row * a.g[g].dst_row + h * a.g[g].dst_head;
-    if (j >= pairs) {
-      j += pairs;
-      dst[j] = src[j];
-      continue;
-    }
-    const float2 cs = turn(p * a.turns[j]);
-    const float c = cs.x * a.gain, s = cs.y * a.gain * a.sign;
-    const int e0 = LAYOUT == PBT_ROTARY_HALF ? j : 2 * j, e1 = LAYOUT == PBT_ROTARY_HALF ? j + pairs : 2 * j + 1;
-    const float u = to_float(src[e0]), v = to_float(src[e1]);
-    set(dst + e0, u * c - v * s);
-    set(dst + e1, v * c + u * s);
+// 16 bytes of elements, or the n < V that there are
+template <class T> struct Unit;
+template <> struct Unit<bf16_t> {
+  static constexpr int V = 8;
+  static __device__ __forceinline__ Vec16 load(const bf16_t* p, int n) { Raw8<bf16_t> r; r.load(p, n); return r.a; }
+  static __device__ __forceinline__ void get(const Vec16& a, float* v) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) { v[2 * q] = __uint_as_float(a.w[q] << 16); v[2 * q + 1] = __uint_as_float(a.w[q] & 0xffff0000u); }
   }
+  static __device__ __forceinline__ Vec16 make(const float* v) { return Vec16{{f2bf_pair(v[0], v[1]), f2bf_pair(v[2], v[3]), f2bf_pair(v[4], v[5]), f2bf_pair(v[6], v[7])}}; }
+  static __device__ __forceinline__ void store_some(bf16_t* p, const Vec16& a, int n) {
+#pragma unroll
+    for (int e = 0; e < V - 1; ++e)
+      if (e < n) p[e] = (bf16_t)(a.w[e >> 1] >> (16 * (e & 1)));
+  }
+};
+template <> struct Unit<float> {
+  static constexpr int V = 4;
+  static __device__ __forceinline__ Vec16 load(const float* p, int n) {
+    if (n >= V) return load16(p);
+    Vec16 a{{0, 0, 0, 0}};
+#pragma unroll
+    for (int e = 0; e < V - 1; ++e)
+      if (e < n) a.w[e] = __float_as_uint(p[e]);
+    return a;
+  }
+  static __device__ __forceinline__ void get(const Vec16& a, float* v) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = __uint_as_float(a.w[q]);
+  }
+  static __device__ __forceinline__ Vec16 make(const float* v) { return Vec16{{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}}; }
+  static __device__ __forceinline__ void store_some(float* p, const Vec16& a, int n) {
+#pragma unroll
+    for (int e = 0; e < V - 1; ++e)
+      if (e < n) p[e] = __uint_as_float(a.w[e]);
+  }
+};
+
+template <class T, bool NT>
+__device__ __forceinline__ void put(T* p, const Vec16& a, int n) {
+  if (n < Unit<T>::V) Unit<T>::store_some(p, a, n);
+  else if (NT) stream16(p, a);
+  else store16(p, a);
+}
+
+// n / d for n d < 2^32, by a product with ceil(2^32 / d) (d = 1: 0)
+__device__ __forceinline__ int quotient(int n, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)n, magic) : n; }
+
+struct Shape {
+  int64_t blocks;            // workgroups of the group of heads
+  int rows, heads;           // of a workgroup
+  int head_blocks;
+  int pair_units, units;     // of a head: units of pairs, then those of the part that is copied
+  uint32_t by_units, by_heads;
+};
+struct Shapes { Shape g[4]; };
+
+// NT: stores that no cache keeps
+template <class T, int LAYOUT, bool NT>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes, int pitch) {
+  extern __shared__ float table[];   // [rows][pitch] cosines, then sines
+  constexpr int V = Unit<T>::V;
+  constexpr int PV = LAYOUT == PBT_ROTARY_HALF ? V : V / 2;   // pairs of a unit
+  // the workgroup's group of heads (one after the other in the grid)
+  Shape w = shapes.g[0];
+  pbt_heads grp = a.g[0];
+  int64_t block = blockIdx.x;
+#pragma unroll
+  for (int g = 1; g < 4; ++g)
+    if (g < a.n_groups && block >= w.blocks) {
+      block -= w.blocks;
+      w = shapes.g[g];
+      grp = a.g[g];
+    }
+  const int pairs = a.rot / 2, head0 = (int)(block % w.head_blocks) * w.heads, heads = min(w.heads, grp.heads - head0);
+  struct Item { const T* src; T* dst; Vec16 x, y; int lds, n; };   // n: pairs (-elements where the unit is copied); lds: the unit's first angle
+  for (int64_t row0 = block / w.head_blocks * w.rows; row0 < a.rows; row0 += w.blocks / w.head_blocks * w.rows) {
+    const int rows = (int)min((int64_t)w.rows, a.rows - row0);
+    // (a workgroup's last block of heads may be short: items are counted over w.heads and those past the end skipped)
+    const int items = rows * w.heads * w.units;
+    auto fetch = [&](int k) {
+      Item it;
+      it.n = 0;
+      if (k >= items) return it;
+      const int q = quotient(k, w.by_units), u = k - q * w.units, r = quotient(q, w.by_heads);
+      const int h = q - r * w.heads;
+      if (h >= heads) return it;
+      it.src = static_cast<const T*>(grp.d_src) + (row0 + r) * grp.src_row + (head0 + h) * grp.src_head;
+      it.dst = static_cast<T*>(grp.d_dst) + (row0 + r) * grp.dst_row + (head0 + h) * grp.dst_head;
+      if (u < w.pair_units) {
+        const int j = u * PV;
+        it.n = min(PV, pairs - j);
+        it.lds = r * pitch + j;
+        if (LAYOUT == PBT_ROTARY_HALF) {
+          it.src += j;
+          it.dst += j;
+          it.x = Unit<T>::load(it.src, it.n);
+          it.y = Unit<T>::load(it.src + pairs, it.n);
+        } else {
+          it.src += 2 * j;
+          it.dst += 2 * j;
+          it.x = Unit<T>::load(it.src, 2 * it.n);
+        }
+      } else {
+        const int e = a.rot + (u - w.pair_units) * V;
+        it.src += e;
+        it.dst += e;
+        it.n = -min(V, a.width - e);
+        it.x = Unit<T>::load(it.src, -it.n);
+      }
+      return it;
+    };
+    Item it = fetch(threadIdx.x);   // (on its way while the angles are formed)
+    for (int k = threadIdx.x; k < rows * pitch; k += 256) {
+      const int r = k / pitch, j = k - r * pitch;
+      if (j < pairs) {
+        const float2 cs = turn((double)position(a, row0 + r) * a.turns[j]);
+        table[k] = cs.x * a.gain;
+        table[w.rows * pitch + k] = cs.y * a.gain * a.sign;
+      }
+    }
+    __syncthreads();
+    for (int k = threadIdx.x;;) {
+      if (it.n < 0) {
+        put<T, NT>(it.dst, it.x, -it.n);
+      } else if (it.n > 0) {
+        float c[PV], s[PV];
+#pragma unroll
+        for (int e = 0; e < PV; ++e) { c[e] = table[it.lds + e]; s[e] = table[w.rows * pitch + it.lds + e]; }
+        float x[V];
+        Unit<T>::get(it.x, x);
+        if (LAYOUT == PBT_ROTARY_HALF) {
+          float y[V];
+          Unit<T>::get(it.y, y);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float u = x[e], v = y[e];
+            x[e] = u * c[e % PV] - v * s[e % PV];
+            y[e] = v * c[e % PV] + u * s[e % PV];
+          }
+          put<T, NT>(it.dst, Unit<T>::make(x), it.n);
+          put<T, NT>(it.dst + pairs, Unit<T>::make(y), it.n);
+        } else {
+#pragma unroll
+          for (int e = 0; e < PV; ++e) {
+            const float u = x[2 * e], v = x[2 * e + 1];
+            x[2 * e] = u * c[e] - v * s[e];
+            x[2 * e + 1] = v * c[e] + u * s[e];
+          }
+          put<T, NT>(it.dst, Unit<T>::make(x), 2 * it.n);
+        }
+      }
+      k += 256;
+      if (k - (int)threadIdx.x >= items) break;
+      it = fetch(k);
+    }
+    __syncthreads();   // (the table is written again)
+  }
+}
+
+uint32_t magic(int d) { return d <= 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
+
+template <class T, int LAYOUT>
+hipError_t launch(const RotaryArgs& a, hipStream_t s) {
+  constexpr int V = Unit<T>::V, PV = LAYOUT == PBT_ROTARY_HALF ? V : V / 2;
+  const int pairs = a.rot / 2, pitch = (pairs + 3) / 4 * 4;
+  Shapes shapes{};
+  int64_t total = 0;
+  int most_rows = 1;
+  for (int g = 0; g < a.n_groups; ++g) {
+    Shape& w = shapes.g[g];
+    w.pair_units = (pairs + PV - 1) / PV;
+    w.units = w.pair_units + (a.g[g].d_src == a.g[g].d_dst ? 0 : (a.width - a.rot + V - 1) / V);
+    w.heads = std::min(std::max(2048 / w.units, 1), (int)a.g[g].heads);
+    w.head_blocks = (a.g[g].heads + w.heads - 1) / w.heads;
+    // A table in LDS serves few rows: the first number of them whose units fill nine tenths of the workgroup's last sweep (else the one that does best), while
+    // four workgroups are left for every compute unit and the table takes at most 16 KB.
+    const int per_row = w.heads * w.units;
+    int64_t limit = std::min<int64_t>(std::min<int64_t>(2048 / pitch, 2048 / per_row + 1), a.rows * w.head_blocks / 1024);
+    int64_t rows = 1;
+    double best = 0.0;
+    for (int64_t r = 1; r <= std::max<int64_t>(limit, 1) && best < 0.9; ++r) {
+      const int64_t n = r * per_row;
+      const double used = (double)n / (double)((n + 255) / 256 * 256);
+      if (used > best) {
+        best = used;
+        rows = r;
+      }
+    }
+    w.rows = (int)rows;
+    w.by_units = magic(w.units);
+    w.by_heads = magic(w.heads);
+    // (a grid holds 2^32 threads: the workgroups of a group take several blocks of rows where there would be more than 2^21 of them)
+    w.blocks = std::min((a.rows + rows - 1) / rows, std::max<int64_t>((1 << 21) / w.head_blocks, 1)) * w.head_blocks;
+    total += w.blocks;
+    most_rows = std::max(most_rows, w.rows);
+  }
+  const size_t lds = (size_t)2 * most_rows * pitch * sizeof(float);
+  int64_t bytes = 0;
+  for (int g = 0; g < a.n_groups; ++g) bytes += a.rows * a.g[g].heads * a.width * (int64_t)sizeof(T);
+  if (bytes > LAST_CACHE) hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, true>), dim3((unsigned)total), dim3(256), lds, s, a, shapes, pitch);
+  else hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, false>), dim3((unsigned)total), dim3(256), lds, s, a, shapes, pitch);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -64,15 +244,8 @@ hipError_t rotary_plan(const RotaryFrequencies& f, int n, double* table, hipStre
 }
 
 hipError_t rotary_apply(const RotaryArgs& a, int layout, int dtype, hipStream_t s) {
-  const dim3 grid((unsigned)(a.rows < (1 << 20) ? a.rows : 1 << 20));
-  if (dtype == PBT_DTYPE_BF16) {
-    if (layout == PBT_ROTARY_HALF) hipLaunchKernelGGL((rotary_kernel<bf16_t, PBT_ROTARY_HALF>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((rotary_kernel<bf16_t, PBT_ROTARY_INTERLEAVED>), grid, dim3(256), 0, s, a);
-  } else {
-    if (layout == PBT_ROTARY_HALF) hipLaunchKernelGGL((rotary_kernel<float, PBT_ROTARY_HALF>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((rotary_kernel<float, PBT_ROTARY_INTERLEAVED>), grid, dim3(256), 0, s, a);
-  }
-  return hipGetLastError();
+  if (dtype == PBT_DTYPE_BF16) return layout == PBT_ROTARY_HALF ? launch<bf16_t, PBT_ROTARY_HALF>(a, s) : launch<bf16_t, PBT_ROTARY_INTERLEAVED>(a, s);
+  return layout == PBT_ROTARY_HALF ? launch<float, PBT_ROTARY_HALF>(a, s) : launch<float, PBT_ROTARY_INTERLEAVED>(a, s);
 }
 
 }  // namespace pbt
