@@ -14,21 +14,22 @@ __global__ __launch_bounds__(256) void rotary_plan_kernel(RotaryFrequencies f, i
   if ((int)threadIdx.x < n) table[threadIdx.x] = f.turns[threadIdx.x];
 }
 
-// cos and sin of p f: the product and the reduction to a quarter turn in double (at position 2^31 the product is good to 1e-7 of a turn, at a million to
-// 1e-10), what is left, at most an eighth of a turn, in float
+// cos and sin of p f, given in turns: the product and the reduction to a quarter turn in double (at position 2^31 the product is good to 1e-7 of a turn, at a
+// million to 1e-10), what is left, x within +-pi/4, in float by the Taylor series: x^11 / 11! and x^12 / 12! are below 2e-9
 __device__ __forceinline__ float2 turn(double turns) {
-  const double q = rint(4.0 * turns);
-  const float r = (float)(4.0 * turns - q) * 0.5f;   // half turns, within +-1/4
-  float s, c;
-  sincospif(r, &s, &c);
-  const int k = (int)(int64_t)q & 3;
+  const double quarters = 4.0 * turns, q = rint(quarters);
+  const float x = (float)(quarters - q) * 1.57079632679489662f;
+  const int k = (int)fma(-4.0, floor(0.25 * q), q);   // q mod 4
+  const float y = x * x;
+  const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -0.166666667f), x);
+  const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -2.75573192e-7f, 2.48015873e-5f), -1.38888889e-3f), 4.16666667e-2f), -0.5f), 1.f);
   const float a = (k & 1) ? s : c, b = (k & 1) ? c : s;   // quarter turns: (c, s), (-s, c), (-c, -s), (s, -c)
   return make_float2(k == 1 || k == 2 ? -a : a, k >= 2 ? -b : b);
 }
 
 __device__ __forceinline__ int64_t position(const RotaryArgs& a, int64_t row) {
   if (a.pos) return a.pos64 ? static_cast<const int64_t*>(a.pos)[row] : (int64_t)static_cast<const int32_t*>(a.pos)[row];
-  return a.start + (a.period > 0 ? row % a.period : row);
+  return a.start + (a.period > 0 ? (int64_t)((uint32_t)row % (uint32_t)a.period) : row);   // (rows and period are below 2^31)
 }
 
 // 16 bytes of elements, or the n < V that there are
@@ -36,11 +37,9 @@ template <class T> struct Unit;
 template <> struct Unit<bf16_t> {
   static constexpr int V = 8;
   static __device__ __forceinline__ Vec16 load(const bf16_t* p, int n) { Raw8<bf16_t> r; r.load(p, n); return r.a; }
-  static __device__ __forceinline__ void get(const Vec16& a, float* v) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) { v[2 * q] = __uint_as_float(a.w[q] << 16); v[2 * q + 1] = __uint_as_float(a.w[q] & 0xffff0000u); }
-  }
-  static __device__ __forceinline__ Vec16 make(const float* v) { return Vec16{{f2bf_pair(v[0], v[1]), f2bf_pair(v[2], v[3]), f2bf_pair(v[4], v[5]), f2bf_pair(v[6], v[7])}}; }
+  // the elements of a word, and back
+  static __device__ __forceinline__ void get(uint32_t w, float* v) { v[0] = __uint_as_float(w << 16); v[1] = __uint_as_float(w & 0xffff0000u); }
+  static __device__ __forceinline__ uint32_t make(const float* v) { return f2bf_pair(v[0], v[1]); }
   static __device__ __forceinline__ void store_some(bf16_t* p, const Vec16& a, int n) {
 #pragma unroll
     for (int e = 0; e < V - 1; ++e)
@@ -57,11 +56,8 @@ template <> struct Unit<float> {
       if (e < n) a.w[e] = __float_as_uint(p[e]);
     return a;
   }
-  static __device__ __forceinline__ void get(const Vec16& a, float* v) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = __uint_as_float(a.w[q]);
-  }
-  static __device__ __forceinline__ Vec16 make(const float* v) { return Vec16{{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}}; }
+  static __device__ __forceinline__ void get(uint32_t w, float* v) { v[0] = __uint_as_float(w); }
+  static __device__ __forceinline__ uint32_t make(const float* v) { return __float_as_uint(v[0]); }
   static __device__ __forceinline__ void store_some(float* p, const Vec16& a, int n) {
 #pragma unroll
     for (int e = 0; e < V - 1; ++e)
@@ -82,7 +78,7 @@ __device__ __forceinline__ int quotient(int n, uint32_t magic) { return magic ? 
 struct Shape {
   int64_t blocks;            // workgroups of the group of heads
   int rows, heads;           // of a workgroup
-  int head_blocks;
+  int head_blocks, row_blocks;   // blocks = head_blocks row_blocks
   int pair_units, units;     // of a head: units of pairs, then those of the part that is copied
   uint32_t by_units, by_heads;
 };
@@ -105,9 +101,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes
       w = shapes.g[g];
       grp = a.g[g];
     }
-  const int pairs = a.rot / 2, head0 = (int)(block % w.head_blocks) * w.heads, heads = min(w.heads, grp.heads - head0);
+  const int pairs = a.rot / 2, head0 = (int)((uint32_t)block % (uint32_t)w.head_blocks) * w.heads, heads = min(w.heads, grp.heads - head0);
   struct Item { const T* src; T* dst; Vec16 x, y; int lds, n; };   // n: pairs (-elements where the unit is copied); lds: the unit's first angle
-  for (int64_t row0 = block / w.head_blocks * w.rows; row0 < a.rows; row0 += w.blocks / w.head_blocks * w.rows) {
+  for (int64_t row0 = (int64_t)((uint32_t)block / (uint32_t)w.head_blocks) * w.rows; row0 < a.rows; row0 += (int64_t)w.row_blocks * w.rows) {
     const int rows = (int)min((int64_t)w.rows, a.rows - row0);
     // (a workgroup's last block of heads may be short: items are counted over w.heads and those past the end skipped)
     const int items = rows * w.heads * w.units;
@@ -157,30 +153,38 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes
       if (it.n < 0) {
         put<T, NT>(it.dst, it.x, -it.n);
       } else if (it.n > 0) {
-        float c[PV], s[PV];
+        // (word by word, so that few angles are in registers at a time)
+        const float *c = table + it.lds, *s = c + w.rows * pitch;
+        constexpr int WE = V / 4;   // elements of a word
 #pragma unroll
-        for (int e = 0; e < PV; ++e) { c[e] = table[it.lds + e]; s[e] = table[w.rows * pitch + it.lds + e]; }
-        float x[V];
-        Unit<T>::get(it.x, x);
+        for (int q = 0; q < 4; ++q) {
+          float x[2], y[2];
+          Unit<T>::get(it.x.w[q], x);
+          if (LAYOUT == PBT_ROTARY_HALF) {
+            Unit<T>::get(it.y.w[q], y);
+#pragma unroll
+            for (int e = 0; e < WE; ++e) {
+              const float u = x[e], v = y[e], ce = c[q * WE + e], se = s[q * WE + e];
+              x[e] = u * ce - v * se;
+              y[e] = v * ce + u * se;
+            }
+            it.y.w[q] = Unit<T>::make(y);
+          } else if (WE == 2) {
+            const float u = x[0], v = x[1], ce = c[q], se = s[q];
+            x[0] = u * ce - v * se;
+            x[1] = v * ce + u * se;
+          } else if (q & 1) {
+            const float u = __uint_as_float(it.x.w[q - 1]), v = x[0], ce = c[q / 2], se = s[q / 2];
+            it.x.w[q - 1] = __float_as_uint(u * ce - v * se);
+            x[0] = v * ce + u * se;
+          }
+          it.x.w[q] = Unit<T>::make(x);
+        }
         if (LAYOUT == PBT_ROTARY_HALF) {
-          float y[V];
-          Unit<T>::get(it.y, y);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float u = x[e], v = y[e];
-            x[e] = u * c[e % PV] - v * s[e % PV];
-            y[e] = v * c[e % PV] + u * s[e % PV];
-          }
-          put<T, NT>(it.dst, Unit<T>::make(x), it.n);
-          put<T, NT>(it.dst + pairs, Unit<T>::make(y), it.n);
+          put<T, NT>(it.dst, it.x, it.n);
+          put<T, NT>(it.dst + pairs, it.y, it.n);
         } else {
-#pragma unroll
-          for (int e = 0; e < PV; ++e) {
-            const float u = x[2 * e], v = x[2 * e + 1];
-            x[2 * e] = u * c[e] - v * s[e];
-            x[2 * e + 1] = v * c[e] + u * s[e];
-          }
-          put<T, NT>(it.dst, Unit<T>::make(x), 2 * it.n);
+          put<T, NT>(it.dst, it.x, 2 * it.n);
         }
       }
       k += 256;
@@ -194,7 +198,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes
 uint32_t magic(int d) { return d <= 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
 
 template <class T, int LAYOUT>
-hipError_t launch(const RotaryArgs& a, hipStream_t s) {
+hipError_t launch(RotaryArgs a, hipStream_t s) {
+  if (a.period >= a.rows) a.period = 0;   // (the rows end before it does)
   constexpr int V = Unit<T>::V, PV = LAYOUT == PBT_ROTARY_HALF ? V : V / 2;
   const int pairs = a.rot / 2, pitch = (pairs + 3) / 4 * 4;
   Shapes shapes{};
@@ -224,7 +229,8 @@ hipError_t launch(const RotaryArgs& a, hipStream_t s) {
     w.by_units = magic(w.units);
     w.by_heads = magic(w.heads);
     // (a grid holds 2^32 threads: the workgroups of a group take several blocks of rows where there would be more than 2^21 of them)
-    w.blocks = std::min((a.rows + rows - 1) / rows, std::max<int64_t>((1 << 21) / w.head_blocks, 1)) * w.head_blocks;
+    w.row_blocks = (int)std::min((a.rows + rows - 1) / rows, std::max<int64_t>((1 << 21) / w.head_blocks, 1));
+    w.blocks = (int64_t)w.row_blocks * w.head_blocks;
     total += w.blocks;
     most_rows = std::max(most_rows, w.rows);
   }
