@@ -1,9 +1,12 @@
 // The gradient norm of every member over a list of tensors, and clipping: norm_i = sqrt(sum g^2), g <- g max_i / norm_i where norm_i > max_i.
 //
-// A member's tensors are laid end to end in units of eight elements (a tensor's last unit may be partly empty), and the units are cut into equal ranges, one
-// workgroup each.  Two launches: partial sums of squares of every range, then every workgroup adds up its member's partial sums (the same order
-// everywhere) and scales its range.  Squares are summed in double: the exact square of a float fits, so nothing overflows or vanishes, and the
-// order, fixed, does not show.
+// A member's tensors are laid end to end in units of eight elements (a tensor's last unit may be partly empty).  Squares are summed in double: the exact
+// square of a float fits, so nothing overflows or vanishes.  Bound by memory: a gradient is read, and where it is clipped read again and written.
+//   Small members: one workgroup a member holds the gradient in registers between the sum and the product, so it is read once, in one launch.
+//   Larger ones: the units are cut into equal ranges, a workgroup each.  One launch leaves every range's sum; in the next every workgroup adds up its
+//   member's sums (the same order everywhere) and scales its range, the ranges that were summed last first: what the cache in front of memory still holds.
+#include <algorithm>
+
 #include "operators.h"
 
 namespace pbt {
@@ -17,107 +20,280 @@ struct ClipTable {
   int64_t start[CLIP_TENSORS + 1];   // first unit of every tensor
   uint64_t bf16;                     // bit k: tensor k is bf16
   int n;
-  int64_t per_chunk;                 // units of a range
 };
+constexpr int TABLE_WORDS = 5 * CLIP_TENSORS + CLIP_TENSORS + 1;
+static_assert(sizeof(ClipTable) == (TABLE_WORDS + 2) * 8, "the table is copied word by word");
 
-__device__ __forceinline__ int tensor_of(const int64_t* start, int n, int64_t u) {
-  int lo = 0, hi = n;   // start[lo] <= u < start[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (start[mid] <= u) lo = mid;
-    else hi = mid;
+// where a thread looks a unit's tensor up: the table's columns, in LDS
+struct Lookup {
+  const uint64_t* w;
+  int n;
+  uint64_t bf16;
+  __device__ __forceinline__ int64_t start(int k) const { return (int64_t)w[5 * CLIP_TENSORS + k]; }
+  __device__ __forceinline__ int of(int64_t u) const {
+    int lo = 0, hi = n;   // start(lo) <= u < start(hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (start(mid) <= u) lo = mid;
+      else hi = mid;
+    }
+    return lo;
   }
-  return lo;
+};
+__device__ __forceinline__ Lookup copy_table(const ClipTable& t, uint64_t* lds) {
+  const uint64_t* words = reinterpret_cast<const uint64_t*>(&t);
+  for (int k = threadIdx.x; k < TABLE_WORDS; k += blockDim.x) lds[k] = words[k];
+  __syncthreads();
+  return Lookup{lds, t.n, t.bf16};
 }
 
+// a unit as it lies in memory
+struct Unit8 { Vec16 a, b; };
+__device__ __forceinline__ void unpack(const Unit8& u, bool half, float* v) {
+  if (half) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) { v[2 * q] = __uint_as_float(u.a.w[q] << 16); v[2 * q + 1] = __uint_as_float(u.a.w[q] & 0xffff0000u); }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) { v[q] = __uint_as_float(u.a.w[q]); v[4 + q] = __uint_as_float(u.b.w[q]); }
+  }
+}
+struct Place { const char* src; char* dst; int n; bool half; };   // of a unit: its addresses and how many of its elements exist
+__device__ __forceinline__ Place place(const Lookup& t, int member, int64_t u) {
+  const int k = t.n > 1 ? t.of(u) : 0;
+  const int64_t e = (u - t.start(k)) * 8, left = (int64_t)t.w[2 * CLIP_TENSORS + k] - e;
+  const bool half = (t.bf16 >> k) & 1;
+  const int shift = half ? 1 : 2;
+  return Place{reinterpret_cast<const char*>(t.w[k]) + ((member * (int64_t)t.w[3 * CLIP_TENSORS + k] + e) << shift),
+               reinterpret_cast<char*>(t.w[CLIP_TENSORS + k]) + ((member * (int64_t)t.w[4 * CLIP_TENSORS + k] + e) << shift), left < 8 ? (int)left : 8, half};
+}
+__device__ __forceinline__ Unit8 read(const Place& p) {
+  Unit8 u;
+  u.b = Vec16{{0, 0, 0, 0}};
+  if (p.half) {
+    Raw8<bf16_t> r;
+    r.load(reinterpret_cast<const bf16_t*>(p.src), p.n);
+    u.a = r.a;
+  } else {
+    Raw8<float> r;
+    r.load(reinterpret_cast<const float*>(p.src), p.n);
+    u.a = r.a;
+    u.b = r.b;
+  }
+  return u;
+}
+__device__ __forceinline__ void write(const Place& p, const float* v) {
+  if (p.half) put8(reinterpret_cast<bf16_t*>(p.dst), v, p.n);
+  else put8(reinterpret_cast<float*>(p.dst), v, p.n);
+}
+__device__ __forceinline__ double squares(const float* v, double acc) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) acc = fma((double)v[q], (double)v[q], acc);
+  return acc;
+}
+
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   double t = 0.0;
-  for (int w = 0; w < (int)blockDim.x / 64; ++w) t += red[w];
-  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) t += red[w];
   return t;
 }
+// the factor of a member of norm n; 1: it stays as it is.  (Rounded to float once, like the norm that is handed out.)
+__device__ __forceinline__ float factor(double n, const float* max_norm) {
+  const double m = (double)*max_norm;
+  return n > m ? (float)(fmax(m, 0.0) / n) : 1.f;
+}
 
-template <bool SCALE>
-__device__ __forceinline__ double walk(const ClipTable& t, int member, int64_t lo, int64_t hi, float c) {
-  double acc = 0.0;
-  for (int64_t u = lo + threadIdx.x; u < hi; u += blockDim.x) {
-    const int k = tensor_of(t.start, t.n, u);
-    const int64_t e = (u - t.start[k]) * 8;
-    const int64_t left = t.len[k] - e;
-    const int n = left < 8 ? (int)left : 8;
-    float v[8];
-    const bool half = (t.bf16 >> k) & 1;
-    if (half) {
-      Raw8<bf16_t> r;
-      r.load(reinterpret_cast<const bf16_t*>(t.src[k]) + member * t.src_stride[k] + e, n);
-      r.get(v);
-    } else {
-      Raw8<float> r;
-      r.load(reinterpret_cast<const float*>(t.src[k]) + member * t.src_stride[k] + e, n);
-      r.get(v);
+// ---- small members: held in registers ----
+// PER units a thread.  (More of them would leave a compute unit one workgroup: 1024 members of 20000 floats take 31 us with 4, 49 with 8.)
+constexpr int HELD_THREADS = 1024;
+template <int PER>
+__global__ __launch_bounds__(HELD_THREADS) void clip_held_kernel(ClipTable table, const float* __restrict__ max_norm, int64_t max_norm_stride, float* __restrict__ norm) {
+  __shared__ uint64_t words[TABLE_WORDS];
+  __shared__ double red[HELD_THREADS / 64];
+  const int i = blockIdx.x;
+  const Lookup t = copy_table(table, words);
+  const int64_t total = t.start(t.n);
+  Unit8 u[PER];
+  uint32_t half = 0;   // bit j: unit j is bf16
+  double s = 0.0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int64_t at = threadIdx.x + j * HELD_THREADS;
+    u[j] = Unit8{};
+    if (at < total) {
+      const Place p = place(t, i, at);
+      u[j] = read(p);
+      half |= p.half ? 1u << j : 0u;
     }
-    if (!SCALE) {
+  }
 #pragma unroll
-      for (int q = 0; q < 8; ++q) acc = fma((double)v[q], (double)v[q], acc);
+  for (int j = 0; j < PER; ++j)
+    if (threadIdx.x + j * HELD_THREADS < total) {
+      float v[8];
+      unpack(u[j], (half >> j) & 1, v);
+      s = squares(v, s);
+    }
+  const double n = sqrt(block_sum<HELD_THREADS>(s, red));
+  if (norm && threadIdx.x == 0) norm[i] = (float)n;
+  if (!max_norm) return;
+  const float c = factor(n, max_norm + i * max_norm_stride);
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int64_t at = threadIdx.x + j * HELD_THREADS;
+    if (at >= total) break;
+    const Place p = place(t, i, at);
+    if (c == 1.f && p.src == p.dst) continue;
+    float v[8];
+    unpack(u[j], p.half, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= c;
+    write(p, v);
+  }
+}
+
+// ---- large members: ranges ----
+// The units [lo, hi) of one tensor as 16-byte vectors, adjacent threads on adjacent vectors, DEEP of them requested at a time; the elements of a last unit that is
+// not whole one by one.  SCALE: dst = c src, NT past the caches; else the sum of squares is returned.
+constexpr int DEEP = 4;
+template <class T, bool SCALE, bool NT>
+__device__ __forceinline__ double along_tensor(const T* src, T* dst, int64_t len, int64_t lo, int64_t hi, float c) {
+  constexpr int V = 16 / (int)sizeof(T);   // elements of a vector
+  double acc = 0.0;
+  auto use = [&](Vec16 x, int64_t at) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (V == 8) {
+        float a = __uint_as_float(x.w[q] << 16), b = __uint_as_float(x.w[q] & 0xffff0000u);
+        if (SCALE) x.w[q] = f2bf_pair(a * c, b * c);
+        else acc = fma((double)b, (double)b, fma((double)a, (double)a, acc));
+      } else {
+        const float a = __uint_as_float(x.w[q]);
+        if (SCALE) x.w[q] = __float_as_uint(a * c);
+        else acc = fma((double)a, (double)a, acc);
+      }
+    }
+    if (SCALE) {
+      if (NT) stream16(dst + at * V, x);
+      else store16(dst + at * V, x);
+    }
+  };
+  const int64_t end = min(hi, len / 8) * (8 / V);
+  int64_t at = lo * (8 / V) + threadIdx.x;
+  for (; at + (DEEP - 1) * 256 < end; at += DEEP * 256) {
+    Vec16 x[DEEP];
+#pragma unroll
+    for (int q = 0; q < DEEP; ++q) x[q] = load16(src + (at + q * 256) * V);
+#pragma unroll
+    for (int q = 0; q < DEEP; ++q) use(x[q], at + q * 256);
+  }
+  for (; at < end; at += 256) use(load16(src + at * V), at);
+  if (hi * 8 > len && threadIdx.x < len % 8) {   // (the range holds the tensor's end)
+    const int64_t e = len / 8 * 8 + threadIdx.x;
+    const float v = V == 8 ? bf2f((bf16_t)src[e]) : (float)src[e];
+    if (!SCALE) acc = fma((double)v, (double)v, acc);
+    else if (V == 8) dst[e] = (T)f2bf(v * c);
+    else dst[e] = (T)(v * c);
+  }
+  return acc;
+}
+
+// the units [lo, hi) of a member: tensor by tensor where the range's tensors are long enough to keep the workgroup busy, else unit by unit
+template <bool SCALE, bool NT>
+__device__ __forceinline__ double walk(const ClipTable& t, uint64_t* words, int member, int64_t lo, int64_t hi, float c) {
+  double acc = 0.0;
+  if (lo >= hi) return acc;
+  // the tensors of the range, by a vote of lanes that look at one tensor each (a loop over the table costs a scalar load after another)
+  const int lane = threadIdx.x & 63;
+  const int64_t start = lane < t.n ? t.start[lane] : INT64_MAX;
+  const int first = __popcll(__ballot(start <= lo)) - 1, last = __popcll(__ballot(start < hi)) - 1;
+  if ((int64_t)(last - first) * 512 <= hi - lo) {
+    for (int k = first; k <= last; ++k) {
+      const int64_t a = max(lo, t.start[k]) - t.start[k], b = min(hi, t.start[k + 1]) - t.start[k];
+      const int64_t from = member * t.src_stride[k], to = member * t.dst_stride[k];
+      if ((t.bf16 >> k) & 1)
+        acc += along_tensor<bf16_t, SCALE, NT>(reinterpret_cast<const bf16_t*>(t.src[k]) + from, reinterpret_cast<bf16_t*>(t.dst[k]) + to, t.len[k], a, b, c);
+      else
+        acc += along_tensor<float, SCALE, NT>(reinterpret_cast<const float*>(t.src[k]) + from, reinterpret_cast<float*>(t.dst[k]) + to, t.len[k], a, b, c);
+    }
+    return acc;
+  }
+  const Lookup l = copy_table(t, words);
+  for (int64_t u = lo + threadIdx.x; u < hi; u += 256) {
+    const Place p = place(l, member, u);
+    float v[8];
+    unpack(read(p), p.half, v);
+    if (SCALE) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= c;
+      write(p, v);
     } else {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] *= c;
-      if (half) put8(reinterpret_cast<bf16_t*>(t.dst[k]) + member * t.dst_stride[k] + e, v, n);
-      else put8(reinterpret_cast<float*>(t.dst[k]) + member * t.dst_stride[k] + e, v, n);
+      acc = squares(v, acc);
     }
   }
   return acc;
 }
 
-__global__ __launch_bounds__(256) void clip_sum_kernel(ClipTable t, double* __restrict__ part, int64_t part_stride, int64_t first) {
-  __shared__ double red[4];
-  const int64_t lo = (int64_t)blockIdx.x * t.per_chunk, hi = min(lo + t.per_chunk, t.start[t.n]);
-  const double s = block_sum(walk<false>(t, blockIdx.y, lo, hi, 0.f), red);
-  if (threadIdx.x == 0) part[blockIdx.y * part_stride + first + blockIdx.x] = s;
-}
-
-// chunk 0 of the first launch writes the norm; max_norm = null: only that
-__global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const double* __restrict__ part, int64_t n_part, const float* __restrict__ max_norm,
-                                                         int64_t max_norm_stride, float* __restrict__ norm, int write_norm, uint64_t in_place) {
+__global__ __launch_bounds__(256) void clip_sum_kernel(ClipTable t, int64_t per_range, double* __restrict__ part, int64_t n_part, int64_t first) {
+  __shared__ uint64_t words[TABLE_WORDS];
   __shared__ double red[4];
   const int i = blockIdx.y;
+  const int64_t lo = (int64_t)blockIdx.x * per_range, hi = min(lo + per_range, t.start[t.n]);
+  const double s = block_sum<256>(walk<false, false>(t, words, i, lo, hi, 0.f), red);
+  if (threadIdx.x == 0) part[i * n_part + first + blockIdx.x] = s;
+}
+
+// write_norm: the first range's workgroup hands the norm out; max_norm = null: only that.  The ranges that were summed last are taken first.
+template <bool NT>
+__global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, int64_t per_range, const double* __restrict__ part, int64_t n_part,
+                                                         const float* __restrict__ max_norm, int64_t max_norm_stride, float* __restrict__ norm, int in_place) {
+  __shared__ uint64_t words[TABLE_WORDS];
+  __shared__ double red[4];
+  const int i = gridDim.y - 1 - blockIdx.y;
+  const int64_t range = gridDim.x - 1 - blockIdx.x;
   double s = 0.0;
   for (int64_t k = threadIdx.x; k < n_part; k += 256) s += part[i * n_part + k];
-  const double n = sqrt(block_sum(s, red));
-  if (write_norm && norm && blockIdx.x == 0 && threadIdx.x == 0) norm[i] = (float)n;
+  const double n = sqrt(block_sum<256>(s, red));
+  if (norm && range == 0 && threadIdx.x == 0) norm[i] = (float)n;
   if (!max_norm) return;
-  const double m = (double)max_norm[i * max_norm_stride];
-  const float c = n > m ? (float)(fmax(m, 0.0) / n) : 1.f;
-  const int64_t lo = (int64_t)blockIdx.x * t.per_chunk, hi = min(lo + t.per_chunk, t.start[t.n]);
-  if (!(n > m) && in_place) return;
-  walk<true>(t, i, lo, hi, c);
+  const float c = factor(n, max_norm + i * max_norm_stride);
+  if (c == 1.f && in_place) return;
+  const int64_t lo = range * per_range, hi = min(lo + per_range, t.start[t.n]);
+  walk<true, NT>(t, words, i, lo, hi, c);
 }
 
 int64_t units(const pbt_grad& g) { return (g.len + 7) / 8; }
-// ranges of a launch over `total` units per member
-int64_t chunks_of(int64_t total, int P) {
-  int64_t most = 4096 / P;
-  if (most < 1) most = 1;
-  const int64_t by_size = (total + 255) / 256;   // at least a unit per thread
-  const int64_t c = by_size < most ? by_size : most;
-  return c < 1 ? 1 : c;
+int64_t units_of(const pbt_grad* g, int k0, int n) {
+  int64_t total = 0;
+  for (int k = k0; k < n && k < k0 + CLIP_TENSORS; ++k) total += units(g[k]);
+  return total;
 }
+// Units a thread holds where members are held, 0: they are not.  A workgroup a member: up to 4 units a thread whatever the number of members (one of 30000 floats:
+// 5 us, 7 in two launches), 8 where there are members for a quarter of the compute units (128 of 60000 floats: 16 us, 20 in two launches; one: 10.5, 7.0).
+int held(const pbt_grad* g, int n, int P) {
+  if (n > CLIP_TENSORS) return 0;
+  const int64_t u = units_of(g, 0, n);
+  return u <= 4 * HELD_THREADS ? 4 : u <= 8 * HELD_THREADS && P >= 64 ? 8 : 0;
+}
+// ranges of a launch over `total` units of each of P members: at least `least` units each, about `grid` workgroups, at most `most` a member
+int64_t ranges_of(int64_t total, int P, int64_t least, int64_t grid, int64_t most) {
+  return std::max<int64_t>(std::min(std::min((total + least - 1) / least, most), std::max<int64_t>(grid / P, 1)), 1);
+}
+int64_t sum_ranges(int64_t total, int P) { return ranges_of(total, P, 256, 2048, 1024); }
+int64_t scale_ranges(int64_t total, int P) { return ranges_of(total, P, 1024, 32768, 32768); }
 int64_t parts(const pbt_grad* g, int n, int P) {
   int64_t sum = 0;
-  for (int k0 = 0; k0 < n; k0 += CLIP_TENSORS) {
-    int64_t total = 0;
-    for (int k = k0; k < n && k < k0 + CLIP_TENSORS; ++k) total += units(g[k]);
-    sum += chunks_of(total, P);
-  }
+  for (int k0 = 0; k0 < n; k0 += CLIP_TENSORS) sum += sum_ranges(units_of(g, k0, n), P);
   return sum;
 }
-ClipTable table(const pbt_grad* g, int k0, int n, int64_t* total, bool* in_place) {
+ClipTable table(const pbt_grad* g, int k0, int n, bool* in_place) {
   ClipTable t;
-  t.n = n - k0 < CLIP_TENSORS ? n - k0 : CLIP_TENSORS;
+  t.n = std::min(n - k0, CLIP_TENSORS);
   t.bf16 = 0;
   *in_place = true;
   int64_t at = 0;
@@ -132,7 +308,11 @@ ClipTable table(const pbt_grad* g, int k0, int n, int64_t* total, bool* in_place
     if (e.d_src != e.d_dst) *in_place = false;
   }
   t.start[t.n] = at;
-  *total = at;
+  for (int k = t.n; k < CLIP_TENSORS; ++k) {
+    t.src[k] = nullptr; t.dst[k] = nullptr;
+    t.len[k] = t.src_stride[k] = t.dst_stride[k] = 0;
+    t.start[k + 1] = at;
+  }
   return t;
 }
 
@@ -141,24 +321,34 @@ ClipTable table(const pbt_grad* g, int k0, int n, int64_t* total, bool* in_place
 size_t clip_work_bytes(const pbt_grad* g, int n, int P) { return (size_t)P * parts(g, n, P) * sizeof(double); }
 
 hipError_t clip_gradients(const pbt_grad* g, int n, int P, const float* max_norm, int64_t max_norm_stride, float* norm, void* work, hipStream_t s) {
+  bool in_place;
+  if (const int per = held(g, n, P)) {
+    const ClipTable t = table(g, 0, n, &in_place);
+    if (per == 4) hipLaunchKernelGGL(clip_held_kernel<4>, dim3(P), dim3(HELD_THREADS), 0, s, t, max_norm, max_norm_stride, norm);
+    else hipLaunchKernelGGL(clip_held_kernel<8>, dim3(P), dim3(HELD_THREADS), 0, s, t, max_norm, max_norm_stride, norm);
+    return hipGetLastError();
+  }
   double* part = static_cast<double*>(work);
   const int64_t n_part = parts(g, n, P);
+  int64_t bytes = 0;
+  for (int k = 0; k < n; ++k) bytes += P * g[k].len * (g[k].dtype == PBT_DTYPE_BF16 ? 2 : 4);
   for (int pass = 0; pass < 2; ++pass) {
     int64_t first = 0;
     for (int k0 = 0; k0 < n; k0 += CLIP_TENSORS) {
-      int64_t total;
-      bool in_place;
-      ClipTable t = table(g, k0, n, &total, &in_place);
-      const int64_t chunks = chunks_of(total, P);
-      t.per_chunk = (total + chunks - 1) / chunks;
+      const ClipTable t = table(g, k0, n, &in_place);
+      const int64_t total = t.start[t.n], ranges = pass == 0 ? sum_ranges(total, P) : max_norm ? scale_ranges(total, P) : 1, per_range = (total + ranges - 1) / ranges;
+      const dim3 grid((unsigned)ranges, P);
       if (pass == 0)
-        hipLaunchKernelGGL(clip_sum_kernel, dim3((unsigned)chunks, P), dim3(256), 0, s, t, part, n_part, first);
-      else if (max_norm || k0 == 0)
-        hipLaunchKernelGGL(clip_scale_kernel, dim3(max_norm ? (unsigned)chunks : 1u, P), dim3(256), 0, s, t, part, n_part, max_norm, max_norm_stride, norm,
-                           k0 == 0, in_place);
+        hipLaunchKernelGGL(clip_sum_kernel, grid, dim3(256), 0, s, t, per_range, part, n_part, first);
+      else if (!max_norm && k0 > 0)
+        break;
+      else if (bytes > LAST_CACHE / 4)
+        hipLaunchKernelGGL(clip_scale_kernel<true>, grid, dim3(256), 0, s, t, per_range, part, n_part, max_norm, max_norm_stride, k0 == 0 ? norm : nullptr, (int)in_place);
+      else
+        hipLaunchKernelGGL(clip_scale_kernel<false>, grid, dim3(256), 0, s, t, per_range, part, n_part, max_norm, max_norm_stride, k0 == 0 ? norm : nullptr, (int)in_place);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
-      first += chunks;
+      first += ranges;
     }
   }
   return hipSuccess;
