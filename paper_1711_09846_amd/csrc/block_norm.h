@@ -1,49 +1,73 @@
 // What both passes of the block norms share (block_norm_forward.hip, block_norm_backward.hip): how a row lies over threads, sums over a row, the gate.
 //
-// A row of d elements lies in the registers of T threads, eight consecutive elements in each of J places: thread l has columns (l + T j) 8 .. + 7.  T = 16
-// (four rows a wavefront) for up to 128 columns, a wavefront for up to 1024, workgroups of 256 and 512 threads for up to 4096 and 8192, so
-// that a row is read once whatever is summed over it.  A workgroup takes a slab of a member's rows; a thread keeps the same
-// columns for all of them, so parameters are read once a slab and their gradients add up in registers.
+// A thread has eight consecutive elements of a row in registers, so that a row is read once whatever is summed over it.  A team of T threads has a row: T = 16
+// (rows of up to 128 elements, four a wavefront), a wavefront (up to 512), or as many wavefronts as the row needs, one workgroup (WIDE, up to 16
+// wavefronts).  A workgroup takes a slab of a member's rows; a thread keeps the same columns for all of them, so parameters are read once a slab and
+// their gradients add up in registers.  The next row is requested as soon as this one's values have been taken over: loads are single instructions without a
+// branch around their results, which the compiler would wait at (with such branches 8191 rows of 5001 took 129 us forward, 94 now).
 #pragma once
+#include <algorithm>
+
 #include "operators.h"
 
 namespace pbt {
 
-struct BlockShape { int T, J; };
-inline BlockShape block_shape(int d) {
-  if (d <= 128) return {16, 1};
-  if (d <= 512) return {64, 1};
-  if (d <= 1024) return {64, 2};
-  if (d <= 2048) return {256, 1};
-  if (d <= 4096) return {256, 2};
-  return {512, 2};
+constexpr int WIDE = 0;   // T of a team that is the whole workgroup
+struct BlockTeam { int T, threads, rows; };   // threads of a workgroup, rows it has at a time
+inline BlockTeam block_team(int d) {
+  if (d <= 128) return {16, 256, 16};
+  if (d <= 512) return {64, 256, 4};
+  return {WIDE, (d + 511) / 512 * 64, 1};
 }
-constexpr int block_threads(int T) { return T < 256 ? 256 : T; }
 
-// sums of two values over the T threads of a row, to all of them; red: 2 x 8 float2 of LDS, ph: which half is used (rows wider than a wavefront: a
-// barrier a call; the halves alternate, so that a wavefront can be one sum ahead of another but not two)
-template <int T>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int& ph) {
-  const auto dpp = [](float v, auto ctrl) { return v + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
-  if (T == 16) {
-    a = dpp(a, std::integral_constant<int, 0x128>()); b = dpp(b, std::integral_constant<int, 0x128>());
-    a = dpp(a, std::integral_constant<int, 0x124>()); b = dpp(b, std::integral_constant<int, 0x124>());
-    a = dpp(a, std::integral_constant<int, 0x4e>()); b = dpp(b, std::integral_constant<int, 0x4e>());
-    a = dpp(a, std::integral_constant<int, 0xb1>()); b = dpp(b, std::integral_constant<int, 0xb1>());
-    return make_float2(a, b);
-  }
-  a = wave_sum(a);
-  b = wave_sum(b);
-  if (T == 64) return make_float2(a, b);
-  float2* r = red + 8 * ph;
-  ph ^= 1;
-  if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = make_float2(a, b);
-  __syncthreads();
-  float2 t = r[0];
-#pragma unroll
-  for (int w = 1; w < T / 64; ++w) { t.x += r[w].x; t.y += r[w].y; }
-  return t;
+// Rows of a slab.  What a slab costs besides its rows (`extra` bytes a column: parameters read, sums written and read again) should be an eighth of what
+// its rows move (`moved` bytes a column and row) and a team should see eight rows, while every compute unit has `resident` workgroups, and there
+// are at most 16 for every compute unit.
+inline int64_t slab_rows(const pbt_block_norm& n, int extra, int moved, int resident) {
+  const BlockTeam t = block_team(n.d);
+  const int64_t all = n.rows * n.P;
+  int64_t rows = std::max<int64_t>((8 * extra + moved - 1) / moved, 8 * t.rows);
+  rows = std::min(rows, (all + 256 * resident - 1) / (256 * resident));   // (rounded up: a few workgroups more than fit would double the time)
+  rows = std::max(rows, (all + 4095) / 4096);
+  rows = (rows + t.rows - 1) / t.rows * t.rows;
+  return std::max<int64_t>(std::min(rows, n.rows), 1);
 }
+
+__device__ __forceinline__ float2 sum16(float2 v) {   // over rows of 16 lanes
+  const auto f = [](float x, auto ctrl) { return x + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+  v.x = f(v.x, std::integral_constant<int, 0x128>()); v.y = f(v.y, std::integral_constant<int, 0x128>());
+  v.x = f(v.x, std::integral_constant<int, 0x124>()); v.y = f(v.y, std::integral_constant<int, 0x124>());
+  v.x = f(v.x, std::integral_constant<int, 0x4e>()); v.y = f(v.y, std::integral_constant<int, 0x4e>());
+  v.x = f(v.x, std::integral_constant<int, 0xb1>()); v.y = f(v.y, std::integral_constant<int, 0xb1>());
+  return v;
+}
+
+// Sums of two values over a team, to all its threads.  WIDE teams: a barrier a sum; wavefronts leave their sums in one of two halves of LDS by turns, so that
+// one wavefront can be a sum ahead of another but not two.
+template <int T> struct TeamSum {
+  __device__ __forceinline__ TeamSum(float2*) {}
+  __device__ __forceinline__ float2 operator()(float a, float b) {
+    if (T == 16) return sum16(make_float2(a, b));
+    return make_float2(wave_sum(a), wave_sum(b));
+  }
+};
+template <> struct TeamSum<WIDE> {
+  float2* red;   // [2][16]
+  int half = 0;
+  __device__ __forceinline__ TeamSum(float2* lds) : red(lds) {
+    if (threadIdx.x < 32) red[threadIdx.x] = make_float2(0.f, 0.f);
+    __syncthreads();
+  }
+  __device__ __forceinline__ float2 operator()(float a, float b) {
+    a = wave_sum(a);
+    b = wave_sum(b);
+    float2* r = red + 16 * half;
+    half ^= 1;
+    if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    return sum16(r[threadIdx.x & 15]);
+  }
+};
 
 // the gate's factor a(g), and a'(g) (SLOPE)
 template <bool SLOPE>
@@ -76,12 +100,28 @@ __device__ __forceinline__ void clear_past(float* v, int n) {
   }
 }
 
-// eight parameters of a member from column c, or `otherwise` where there are none; zero past the row's end
-__device__ __forceinline__ void param8(const float* p, int64_t stride, int member, int c, int n, float otherwise, float* v) {
+// a row's eight elements; TINY: rows of fewer than eight elements
+template <bool TINY, class T>
+__device__ __forceinline__ void load_row(Raw8<T>& r, const T* p, int n) {
+  if (TINY) r.load(p, n);
+  else r.load_end(p, n);
+}
+template <bool TINY, class T>
+__device__ __forceinline__ void get_row(const Raw8<T>& r, float* v, int n) {
+  if (TINY) r.get(v);
+  else get_end(r, v, n);
+}
+
+// Eight parameters of a member from column c, or `otherwise` where there are none; zero past the row's end.  All of a kernel's are requested before the first
+// is looked at.
+template <bool TINY>
+__device__ __forceinline__ void load_param(Raw8<float>& r, const float* p, int64_t stride, int member, int c, int n) {
+  if (p) load_row<TINY>(r, p + member * stride + c, n);
+}
+template <bool TINY>
+__device__ __forceinline__ void get_param(const Raw8<float>& r, const float* p, int n, float otherwise, float* v) {
   if (p) {
-    Raw8<float> r;
-    r.load(p + member * stride + c, n);
-    r.get(v);
+    get_row<TINY>(r, v, n);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = otherwise;
@@ -91,32 +131,25 @@ __device__ __forceinline__ void param8(const float* p, int64_t stride, int membe
 
 template <class T> __device__ __forceinline__ T* row_at(const pbt_rows& m, int64_t row) { return static_cast<T*>(m.d) + row * m.pitch; }
 
-// statistics of a row in registers: mean (LAYER; else 0) and 1 / sqrt(variance or mean square + eps); the values become (v - mean).  The variance is summed
-// over the differences, a second sum: no cancellation.  (Divisions: the mean of a row of equal
-// values is that value, which a reciprocal's rounding would not give.)
-template <int T, int J>
-__device__ __forceinline__ float2 row_stats(float (*v)[8], const int* n, int kind, float d, float eps, float2* red, int& ph) {
+// Statistics of a row: mean (LAYER; else 0) and 1 / sqrt(variance or mean square + eps); the values become v - mean.  The variance is summed over the
+// differences, a second sum: no cancellation.  (Divisions: the mean of a row of equal values is that value, which a reciprocal's rounding would not
+// give.)
+template <class Sum>
+__device__ __forceinline__ float2 row_stats(float* v, int n, int kind, float d, float eps, Sum& sum) {
   float mean = 0.f;
   if (kind == PBT_NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int e = 0; e < 8; ++e) s += v[e];
+    mean = sum(s, 0.f).x / d;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += v[j][e];
-    mean = row_sum2<T>(s, 0.f, red, ph).x / d;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[j][e] -= mean;
-      clear_past(v[j], n[j]);
-    }
+    for (int e = 0; e < 8; ++e) v[e] -= mean;
+    clear_past(v, n);
   }
   float q = 0.f;
 #pragma unroll
-  for (int j = 0; j < J; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q = fmaf(v[j][e], v[j][e], q);
-  return make_float2(mean, rsqrtf(row_sum2<T>(q, 0.f, red, ph).x / d + eps));
+  for (int e = 0; e < 8; ++e) q = fmaf(v[e], v[e], q);
+  return make_float2(mean, rsqrtf(sum(q, 0.f).x / d + eps));
 }
 
 }  // namespace pbt

@@ -1,191 +1,228 @@
 // Block norms, backward, one pass over everything and a short sum of the parameters' gradients:
 //   t = dout + N_pre^T(dz),  dx = alpha t,  v = beta a(gate) t,  dgate = beta a'(gate) u t,  dy = N_post^T(v)
 //   N^T(w) = spread^-1 (w g - mean(w g) - hat mean(w g hat))   (RMS: without the first mean)
-// u and out are formed again from y, x and the gate.  dz hat, dz, v hat, v (and u t for a gate vector) are summed over a slab's rows in registers; the
-// slabs' sums go to `part`, and a second launch adds them in slab order.
+// u and out are formed again from y, x and the gate.  dz hat, dz, v hat, v (and dgate for a gate vector) are summed over a slab's rows in registers; the
+// slabs' sums go to `part`, and a second launch adds them in slab order.  The parameters wait in LDS: a compute unit gets some eight bytes a cycle from memory
+// and 128 from LDS, registers are what limits how many rows are on their way.
+#include <algorithm>
+#include <type_traits>
 
 #include "block_norm.h"
+#include "gemm_common.h"
 
 namespace pbt {
 namespace {
 
-constexpr int SUMS = 5;   // post gain, post bias, pre gain, pre bias, gate vector
+constexpr int SUMS = 5;     // post gain, post bias, pre gain, pre bias, gate vector
+constexpr int PARAMS = 4;   // post gain, post bias, pre gain, the gate's factor
 
-template <class A, class R, int T, int J>
-__global__ __launch_bounds__(block_threads(T)) void block_backward_kernel(BlockArgs a, int64_t rows_per_slab) {
-  __shared__ float2 red[16];
-  __shared__ float acc_lds[T <= 64 ? SUMS * T * J * 8 : 1];
-  constexpr int GROUPS = block_threads(T) / T;
-  const int i = blockIdx.y, l = threadIdx.x % T, group = threadIdx.x / T;
+__device__ __forceinline__ void from_lds(const float4* lds, int stride, int which, int l, float* v) {
+  const float4 a = lds[(2 * which) * stride + l], b = lds[(2 * which + 1) * stride + l];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void to_lds(float4* lds, int stride, int which, int l, const float* v) {
+  lds[(2 * which) * stride + l] = make_float4(v[0], v[1], v[2], v[3]);
+  lds[(2 * which + 1) * stride + l] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+template <class A, class R, int T, int MOST, bool TINY>
+__global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64_t rows_per_slab) {
+  extern __shared__ float4 lds[];   // [PARAMS][2][threads of a team], then the team's sums
+  constexpr int ROWS = T == WIDE ? 1 : 256 / T;
+  const int team = T == WIDE ? (int)blockDim.x : T;
+  __shared__ float2 red[32];
+  TeamSum<T> sum(red);
+  const int i = blockIdx.y, l = T == WIDE ? threadIdx.x : threadIdx.x % T, group = T == WIDE ? 0 : threadIdx.x / T;
   const pbt_block_norm& k = a.n;
   const float inv_d = 1.f / (float)k.d;
-  int ph = 0;
-  int n[J];
-  float g1[J][8], b1[J][8], g2[J][8], gv[J][8];
-  float acc[SUMS][J][8];
+  const int c = l * 8, n = k.d - c;
+  const bool rows_gate = k.gate == PBT_GATE_ROWS, has_dz = a.dz.d != nullptr, has_dout = a.dout.d != nullptr;
+  const int64_t r_end = min(k.rows, (int64_t)(blockIdx.x + 1) * rows_per_slab);
+  Raw8<A> y, gate, dzr;
+  Raw8<R> x, dout;
+  float4 st_next;
+  auto fetch = [&](int64_t r) {
+    const int64_t row = i * k.rows + r;
+    st_next = reinterpret_cast<const float4*>(a.stats)[row];
+    load_row<TINY>(y, row_at<A>(a.y, row) + c, n);
+    load_row<TINY>(x, row_at<R>(a.x, row) + c, n);
+    if (rows_gate) load_row<TINY>(gate, row_at<A>(a.gate, row) + c, n);
+    if (has_dz) load_row<TINY>(dzr, row_at<A>(a.dz, row) + c, n);
+  };
+  auto fetch_dout = [&](int64_t r) {
+    if (has_dout) load_row<TINY>(dout, row_at<R>(a.dout, i * k.rows + r) + c, n);
+  };
+  int64_t r = blockIdx.x * rows_per_slab + group;
+  if (r < r_end) {
+    fetch(r);
+    fetch_dout(r);
+  }
+  if (group == 0) {
+    Raw8<float> raw[4];
+    const float* const at[4] = {a.p.post_gain, a.p.post_bias, a.p.pre_gain, k.gate == PBT_GATE_VECTOR ? a.p.gate : nullptr};
+    float p[8];
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int c = (l + T * j) * 8;
-    n[j] = k.d - c;
-    param8(a.p.post_gain, a.p.stride, i, c, n[j], 1.f, g1[j]);
-    param8(a.p.post_bias, a.p.stride, i, c, n[j], 0.f, b1[j]);
-    param8(a.p.pre_gain, a.p.stride, i, c, n[j], 1.f, g2[j]);
+    for (int q = 0; q < 4; ++q) load_param<TINY>(raw[q], at[q], a.p.stride, i, c, n);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      get_param<TINY>(raw[q], at[q], n, q == 1 ? 0.f : 1.f, p);
+      to_lds(lds, team, q, l, p);
+    }
     if (k.gate == PBT_GATE_VECTOR) {
       float g[8];
-      param8(a.p.gate, a.p.stride, i, c, n[j], 0.f, g);
-      gate8<false>(k.gate_act, g, gv[j], nullptr);
+      get_param<TINY>(raw[3], at[3], n, 0.f, g);
+      gate8<false>(k.gate_act, g, p, nullptr);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) gv[j][e] = 1.f;
+      for (int e = 0; e < 8; ++e) p[e] = 1.f;
     }
-#pragma unroll
-    for (int q = 0; q < SUMS; ++q)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[q][j][e] = 0.f;
+    to_lds(lds, team, 3, l, p);
   }
-  const int64_t r_end = min(k.rows, (int64_t)(blockIdx.x + 1) * rows_per_slab);
-  for (int64_t r = blockIdx.x * rows_per_slab + group; r < r_end; r += GROUPS) {
+  __syncthreads();
+  float acc[SUMS][8];
+#pragma unroll
+  for (int q = 0; q < SUMS; ++q)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[q][e] = 0.f;
+  for (; r < r_end; r += ROWS) {
     const int64_t row = i * k.rows + r;
-    const float4 st = reinterpret_cast<const float4*>(a.stats)[row];
-    float yh[J][8], xh[J][8], dz[J][8], t[J][8], f[J][8], df[J][8];
-    Raw8<A> y[J], gate[J], dzr[J];
-    Raw8<R> x[J], dout[J];
+    const float4 st = st_next;
+    float yh[8], xh[8], t[8], f[8], df[8], p[8], q[8];
+    get_row<TINY>(y, yh, n);
+    get_row<TINY>(x, xh, n);
+    if (rows_gate) {
+      get_row<TINY>(gate, p, n);
+      gate8<true>(k.gate_act, p, f, df);
+    } else {
+      from_lds(lds, team, 3, l, f);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = (l + T * j) * 8;
-      y[j].load(row_at<A>(a.y, row) + c, n[j]);
-      x[j].load(row_at<R>(a.x, row) + c, n[j]);
-      if (k.gate == PBT_GATE_ROWS) gate[j].load(row_at<A>(a.gate, row) + c, n[j]);
-      if (a.dz.d) dzr[j].load(row_at<A>(a.dz, row) + c, n[j]);
-      if (a.dout.d) dout[j].load(row_at<R>(a.dout, row) + c, n[j]);
+      for (int e = 0; e < 8; ++e) df[e] = 1.f;
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) yh[e] = (yh[e] - st.x) * st.y;
+    float u[8];
+    if (k.post != PBT_NORM_NONE) {
+      from_lds(lds, team, 0, l, p);
+      from_lds(lds, team, 1, l, q);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = fmaf(yh[e], p[e], q[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = yh[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      xh[e] = (fmaf(k.beta * f[e], u[e], k.alpha * xh[e]) - st.z) * st.w;
+      df[e] *= u[e];
+    }
+    clear_past(yh, n);
+    clear_past(xh, n);
     float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      float u[8];
-      y[j].get(yh[j]);
-      x[j].get(xh[j]);
-      if (k.gate == PBT_GATE_ROWS) {
-        float g[8];
-        gate[j].get(g);
-        gate8<true>(k.gate_act, g, f[j], df[j]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { f[j][e] = gv[j][e]; df[j][e] = 1.f; }
-      }
+    if (has_dz) {
+      float dz[8];
+      get_row<TINY>(dzr, dz, n);
+      from_lds(lds, team, 2, l, p);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        yh[j][e] = (yh[j][e] - st.x) * st.y;
-        u[e] = k.post != PBT_NORM_NONE ? fmaf(yh[j][e], g1[j][e], b1[j][e]) : yh[j][e];
-        const float o = fmaf(k.beta * f[j][e], u[e], k.alpha * xh[j][e]);
-        xh[j][e] = (o - st.z) * st.w;
-        df[j][e] *= u[e];
-      }
-      clear_past(yh[j], n[j]);
-      clear_past(xh[j], n[j]);
-      if (a.dz.d) {
-        dzr[j].get(dz[j]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float w = dz[j][e] * g2[j][e];
-          s1 += w;
-          s2 = fmaf(w, xh[j][e], s2);
-          t[j][e] = w;
-          acc[2][j][e] = fmaf(dz[j][e], xh[j][e], acc[2][j][e]);
-          acc[3][j][e] += dz[j][e];
-        }
+        t[e] = dz[e] * p[e];
+        s1 += t[e];
+        s2 = fmaf(t[e], xh[e], s2);
+        acc[2][e] = fmaf(dz[e], xh[e], acc[2][e]);
+        acc[3][e] += dz[e];
       }
     }
-    if (a.dz.d) {
-      const float2 m = row_sum2<T>(s1, s2, red, ph);
+    if (r + ROWS < r_end) fetch(r + ROWS);   // (on its way while this row is reduced)
+    if (has_dz) {
+      const float2 m = sum(s1, s2);
       s1 = k.pre == PBT_NORM_LAYER ? m.x * inv_d : 0.f;
       s2 = m.y * inv_d;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = st.w * (t[e] - s1 - xh[e] * s2);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = 0.f;
     }
-    float q1 = 0.f, q2 = 0.f;
+    if (has_dout) {
+      float dv[8];
+      get_row<TINY>(dout, dv, n);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = (l + T * j) * 8;
-      float dx[8], dg[8], dv[8];
-      if (a.dout.d) dout[j].get(dv);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float s = a.dz.d ? st.w * (t[j][e] - s1 - xh[j][e] * s2) : 0.f;
-        if (a.dout.d) s += dv[e];
-        t[j][e] = s;
-      }
-      clear_past(t[j], n[j]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float s = t[j][e];
-        dx[e] = k.alpha * s;
-        dg[e] = k.beta * s * df[j][e];   // a'(g) u t
-        acc[4][j][e] += dg[e];
-        const float v = k.beta * f[j][e] * s;
-        acc[0][j][e] = fmaf(v, yh[j][e], acc[0][j][e]);
-        acc[1][j][e] += v;
-        const float w = v * g1[j][e];
-        q1 += w;
-        q2 = fmaf(w, yh[j][e], q2);
-        t[j][e] = k.post != PBT_NORM_NONE ? w : v;
-      }
-      put8(row_at<R>(a.dx, row) + c, dx, n[j]);
-      if (k.gate == PBT_GATE_ROWS) put8(row_at<A>(a.dgate, row) + c, dg, n[j]);
+      for (int e = 0; e < 8; ++e) t[e] += dv[e];
     }
+    if (r + ROWS < r_end) fetch_dout(r + ROWS);
+    clear_past(t, n);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      xh[e] = k.alpha * t[e];             // dx
+      df[e] = k.beta * t[e] * df[e];      // dgate
+      t[e] = k.beta * f[e] * t[e];        // v
+      acc[4][e] += df[e];
+      acc[0][e] = fmaf(t[e], yh[e], acc[0][e]);
+      acc[1][e] += t[e];
+    }
+    put8(row_at<R>(a.dx, row) + c, xh, n);
+    if (rows_gate) put8(row_at<A>(a.dgate, row) + c, df, n);
     if (k.post != PBT_NORM_NONE) {
-      const float2 m = row_sum2<T>(q1, q2, red, ph);
+      from_lds(lds, team, 0, l, p);
+      float q1 = 0.f, q2 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        t[e] *= p[e];
+        q1 += t[e];
+        q2 = fmaf(t[e], yh[e], q2);
+      }
+      const float2 m = sum(q1, q2);
       q1 = k.post == PBT_NORM_LAYER ? m.x * inv_d : 0.f;
       q2 = m.y * inv_d;
-    }
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = (l + T * j) * 8;
-      if (k.post != PBT_NORM_NONE) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[j][e] = st.y * (t[j][e] - q1 - yh[j][e] * q2);
-      }
-      put8(row_at<A>(a.dy, row) + c, t[j], n[j]);
+      for (int e = 0; e < 8; ++e) t[e] = st.y * (t[e] - q1 - yh[e] * q2);
     }
+    put8(row_at<A>(a.dy, row) + c, t, n);
   }
   // the gate vector's slope is the same for all rows
   if (k.gate == PBT_GATE_VECTOR) {
+    float g[8], f[8], df[8];
+    Raw8<float> raw;
+    load_param<TINY>(raw, a.p.gate, a.p.stride, i, c, n);
+    get_param<TINY>(raw, a.p.gate, n, 0.f, g);
+    gate8<true>(k.gate_act, g, f, df);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      float g[8], f[8], df[8];
-      param8(a.p.gate, a.p.stride, i, (l + T * j) * 8, n[j], 0.f, g);
-      gate8<true>(k.gate_act, g, f, df);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[4][j][e] *= df[e];
-    }
+    for (int e = 0; e < 8; ++e) acc[4][e] *= df[e];
   }
   float* const* grads = &a.g.post_gain;
   float* part = a.part + ((int64_t)i * gridDim.x + blockIdx.x) * SUMS * k.d;
-  if (T <= 64) {
-    // groups of a workgroup take turns
-    for (int turn = 0; turn < GROUPS; ++turn) {
-      if (group == turn) {
+  if (T != WIDE) {
+    // the teams of a workgroup add theirs up: those of a wavefront across its lanes, then the wavefronts in turn
+    if (T == 16) {
 #pragma unroll
-        for (int q = 0; q < SUMS; ++q)
+      for (int q = 0; q < SUMS; ++q)
 #pragma unroll
-          for (int j = 0; j < J; ++j)
+        for (int e = 0; e < 8; ++e) {
+          acc[q][e] += __shfl_xor(acc[q][e], 16);
+          acc[q][e] += __shfl_xor(acc[q][e], 32);
+        }
+    }
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();   // (the parameters in LDS have been used)
+    for (int turn = 0; turn < 4; ++turn) {
+      if (wave == turn && (threadIdx.x & 63) < T) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float* p = acc_lds + (q * J + j) * T * 8 + l * 8 + e;
-              *p = turn == 0 ? acc[q][j][e] : *p + acc[q][j][e];
-            }
+        for (int q = 0; q < SUMS; ++q) {
+          float v[8];
+          if (turn > 0) {
+            from_lds(lds, team, q, l, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[q][e] = v[e] + acc[q][e];
+          }
+          if (turn < 3) to_lds(lds, team, q, l, acc[q]);
+          else if (grads[q]) put8(part + q * k.d + c, acc[q], n);
+        }
       }
       __syncthreads();
     }
-#pragma unroll
-    for (int q = 0; q < SUMS; ++q)
-      if (grads[q])
-        for (int c = threadIdx.x; c < k.d; c += block_threads(T)) part[q * k.d + c] = acc_lds[q * J * T * 8 + c];
   } else {
 #pragma unroll
     for (int q = 0; q < SUMS; ++q)
-      if (grads[q]) {
-#pragma unroll
-        for (int j = 0; j < J; ++j) put8(part + q * k.d + (l + T * j) * 8, acc[q][j], n[j]);
-      }
+      if (grads[q]) put8(part + q * k.d + c, acc[q], n);
   }
 }
 
@@ -198,33 +235,53 @@ __global__ __launch_bounds__(256) void block_param_kernel(const float* __restric
   const int c = blockIdx.x * 64 + cl;
   const int per = (slabs + 3) / 4, k_end = min(slabs, (grp + 1) * per);
   float acc = 0.f;
-  if (c < d)
-    for (int k = grp * per; k < k_end; ++k) acc += part[((int64_t)(i * (int64_t)slabs + k) * SUMS + blockIdx.y) * d + c];
+  if (c < d) {
+    const float* __restrict__ p = part + ((int64_t)i * slabs * SUMS + blockIdx.y) * d + c;
+    for (int k = grp * per; k < k_end; k += 8) {   // (eight loads on their way)
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = k + q < k_end ? p[(int64_t)(k + q) * SUMS * d] : 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) acc += v[q];
+    }
+  }
   red[grp][cl] = acc;
   __syncthreads();
   if (grp == 0 && c < d) out[i * g.stride + c] = ((red[0][cl] + red[1][cl]) + red[2][cl]) + red[3][cl];
 }
 
-int64_t slabs_of(const pbt_block_norm& n) {
-  const BlockShape b = block_shape(n.d);
-  const int groups = block_threads(b.T) / b.T;
-  const int64_t most = 1024 / n.P + 1;
-  const int64_t s = (n.rows + groups - 1) / groups;
-  return s < most ? s : most;
+// (every gradient counted: the working memory does not depend on which are asked for)
+int64_t rows_per_slab(const pbt_block_norm& n) {
+  const int a = n.dtype == PBT_DTYPE_BF16 ? 2 : 4, r = n.res_dtype == PBT_DTYPE_BF16 ? 2 : 4;
+  const int norms = (n.post != PBT_NORM_NONE) + (n.pre != PBT_NORM_NONE), sums = 2 * norms + (n.gate == PBT_GATE_VECTOR);
+  const int moved = (n.pre != PBT_NORM_NONE ? 3 : 2) * a + (n.gate == PBT_GATE_ROWS ? 2 * a : 0) + 3 * r;
+  return slab_rows(n, 4 * sums + 8 * sums, moved, std::max(8 / (block_team(n.d).threads / 64), 1));
 }
+int64_t slabs_of(const pbt_block_norm& n) { return (n.rows + rows_per_slab(n) - 1) / rows_per_slab(n); }
 
-template <class A, class R, int T, int J>
-void launch(const BlockArgs& a, int64_t slabs, hipStream_t s) {
-  const int64_t rows_per_slab = (a.n.rows + slabs - 1) / slabs;
-  hipLaunchKernelGGL((block_backward_kernel<A, R, T, J>), dim3((unsigned)slabs, a.n.P), dim3(block_threads(T)), 0, s, a, rows_per_slab);
+// more than 64 KB of LDS need a permission, once on every device (wide teams have 72 to 128 KB, whose compute unit has no room for a second of them anyway)
+template <class A, class R, int MOST>
+hipError_t launch_wide(const BlockArgs& a, int64_t per_slab, dim3 grid, dim3 block, size_t lds, hipStream_t s) {
+  if (lds > 64 * 1024) {
+    const hipError_t e = allow_lds<&block_backward_kernel<A, R, WIDE, MOST, false>>(128 * 1024);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((block_backward_kernel<A, R, WIDE, MOST, false>), grid, block, lds, s, a, per_slab);
+  return hipGetLastError();
 }
 template <class A, class R>
-void by_width(const BlockArgs& a, int64_t slabs, hipStream_t s) {
-  const BlockShape b = block_shape(a.n.d);
-  if (b.T == 16) launch<A, R, 16, 1>(a, slabs, s);
-  else if (b.T == 64) b.J == 1 ? launch<A, R, 64, 1>(a, slabs, s) : launch<A, R, 64, 2>(a, slabs, s);
-  else if (b.T == 256) b.J == 1 ? launch<A, R, 256, 1>(a, slabs, s) : launch<A, R, 256, 2>(a, slabs, s);
-  else launch<A, R, 512, 2>(a, slabs, s);
+hipError_t launch(const BlockArgs& a, int64_t slabs, hipStream_t s) {
+  const BlockTeam t = block_team(a.n.d);
+  const int64_t per_slab = rows_per_slab(a.n);
+  const dim3 grid((unsigned)slabs, a.n.P), block(t.threads);
+  const size_t lds = (size_t)(t.T == WIDE ? PARAMS : SUMS) * 2 * (t.T == WIDE ? t.threads : t.T) * sizeof(float4);
+  if (a.n.d < 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, true>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 16) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, false>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 64) hipLaunchKernelGGL((block_backward_kernel<A, R, 64, 256, false>), grid, block, lds, s, a, per_slab);
+  else if (t.threads <= 512) return launch_wide<A, R, 512>(a, per_slab, grid, block, lds, s);
+  else if (t.threads <= 768) return launch_wide<A, R, 768>(a, per_slab, grid, block, lds, s);
+  else return launch_wide<A, R, 1024>(a, per_slab, grid, block, lds, s);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -235,9 +292,8 @@ hipError_t block_norm_backward(const BlockArgs& a, hipStream_t s) {
   const int64_t slabs = slabs_of(a.n);
   if (slabs > 0) {
     const bool act16 = a.n.dtype == PBT_DTYPE_BF16, res16 = a.n.res_dtype == PBT_DTYPE_BF16;
-    if (act16) res16 ? by_width<bf16_t, bf16_t>(a, slabs, s) : by_width<bf16_t, float>(a, slabs, s);
-    else res16 ? by_width<float, bf16_t>(a, slabs, s) : by_width<float, float>(a, slabs, s);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = act16 ? (res16 ? launch<bf16_t, bf16_t>(a, slabs, s) : launch<bf16_t, float>(a, slabs, s))
+                               : (res16 ? launch<float, bf16_t>(a, slabs, s) : launch<float, float>(a, slabs, s));
     if (e != hipSuccess) return e;
   }
   const pbt_block_params& g = a.g;

@@ -1,113 +1,105 @@
 // Block norms, forward: u = N_post(y), out = alpha x + beta a(gate) u, z = N_pre(out) in one pass over y, x and the gate.
+#include <algorithm>
+#include <type_traits>
 
 #include "block_norm.h"
 
 namespace pbt {
 namespace {
 
-template <class A, class R, int T, int J>
-__global__ __launch_bounds__(block_threads(T)) void block_forward_kernel(BlockArgs a, int64_t rows_per_slab) {
-  __shared__ float2 red[16];
-  constexpr int GROUPS = block_threads(T) / T;   // rows at a time
-  const int i = blockIdx.y, l = threadIdx.x % T, group = threadIdx.x / T;
+template <class A, class R, int T, int MOST, bool TINY>
+__global__ __launch_bounds__(MOST) void block_forward_kernel(BlockArgs a, int64_t rows_per_slab) {
+  __shared__ float2 red[32];
+  TeamSum<T> sum(red);
+  constexpr int ROWS = T == WIDE ? 1 : 256 / T;   // rows at a time
+  const int i = blockIdx.y, l = T == WIDE ? threadIdx.x : threadIdx.x % T, group = T == WIDE ? 0 : threadIdx.x / T;
   const pbt_block_norm& k = a.n;
   const float d = (float)k.d;
-  int ph = 0;
-  int n[J];
-  float g1[J][8], b1[J][8], g2[J][8], b2[J][8], gv[J][8];
+  const int c = l * 8, n = k.d - c;   // the thread's columns, how many of them there are (n <= 0: none)
+  const bool rows_gate = k.gate == PBT_GATE_ROWS;
+  const int64_t r_end = min(k.rows, (int64_t)(blockIdx.x + 1) * rows_per_slab);
+  Raw8<A> y, gate;
+  Raw8<R> x;
+  auto fetch = [&](int64_t r) {
+    const int64_t row = i * k.rows + r;
+    load_row<TINY>(y, row_at<A>(a.y, row) + c, n);
+    load_row<TINY>(x, row_at<R>(a.x, row) + c, n);
+    if (rows_gate) load_row<TINY>(gate, row_at<A>(a.gate, row) + c, n);
+  };
+  int64_t r = blockIdx.x * rows_per_slab + group;
+  if (r < r_end) fetch(r);   // (on its way while the parameters are read)
+  float g1[8], b1[8], g2[8], b2[8], f[8];
+  {
+    Raw8<float> p[5];
+    const float* const at[5] = {a.p.post_gain, a.p.post_bias, a.p.pre_gain, a.p.pre_bias, k.gate == PBT_GATE_VECTOR ? a.p.gate : nullptr};
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int c = (l + T * j) * 8;
-    n[j] = k.d - c;
-    param8(a.p.post_gain, a.p.stride, i, c, n[j], 1.f, g1[j]);
-    param8(a.p.post_bias, a.p.stride, i, c, n[j], 0.f, b1[j]);
-    param8(a.p.pre_gain, a.p.stride, i, c, n[j], 1.f, g2[j]);
-    param8(a.p.pre_bias, a.p.stride, i, c, n[j], 0.f, b2[j]);
+    for (int q = 0; q < 5; ++q) load_param<TINY>(p[q], at[q], a.p.stride, i, c, n);
+    get_param<TINY>(p[0], at[0], n, 1.f, g1);
+    get_param<TINY>(p[1], at[1], n, 0.f, b1);
+    get_param<TINY>(p[2], at[2], n, 1.f, g2);
+    get_param<TINY>(p[3], at[3], n, 0.f, b2);
     if (k.gate == PBT_GATE_VECTOR) {
       float g[8];
-      param8(a.p.gate, a.p.stride, i, c, n[j], 0.f, g);
-      gate8<false>(k.gate_act, g, gv[j], nullptr);
+      get_param<TINY>(p[4], at[4], n, 0.f, g);
+      gate8<false>(k.gate_act, g, f, nullptr);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) gv[j][e] = 1.f;
+      for (int e = 0; e < 8; ++e) f[e] = 1.f;
     }
   }
-  const int64_t r_end = min(k.rows, (int64_t)(blockIdx.x + 1) * rows_per_slab);
-  for (int64_t r = blockIdx.x * rows_per_slab + group; r < r_end; r += GROUPS) {
+  for (; r < r_end; r += ROWS) {
     const int64_t row = i * k.rows + r;
-    float u[J][8], o[J][8];
-    Raw8<A> gate[J];
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = (l + T * j) * 8;
-      Raw8<A> y;
-      Raw8<R> x;
-      y.load(row_at<A>(a.y, row) + c, n[j]);
-      x.load(row_at<R>(a.x, row) + c, n[j]);
-      if (k.gate == PBT_GATE_ROWS) gate[j].load(row_at<A>(a.gate, row) + c, n[j]);
-      y.get(u[j]);
-      x.get(o[j]);
+    float u[8], o[8];
+    get_row<TINY>(y, u, n);
+    get_row<TINY>(x, o, n);
+    if (rows_gate) {
+      float g[8];
+      get_row<TINY>(gate, g, n);
+      gate8<false>(k.gate_act, g, f, nullptr);
     }
+    if (r + ROWS < r_end) fetch(r + ROWS);   // (on its way while this row is reduced)
     float2 s1 = make_float2(0.f, 1.f), s2 = make_float2(0.f, 1.f);
-    if (k.post != PBT_NORM_NONE) s1 = row_stats<T, J>(u, n, k.post, d, k.eps, red, ph);
+    if (k.post != PBT_NORM_NONE) {
+      s1 = row_stats(u, n, k.post, d, k.eps, sum);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = (l + T * j) * 8;
-      float f[8];
-      if (k.gate == PBT_GATE_ROWS) {
-        float g[8];
-        gate[j].get(g);
-        gate8<false>(k.gate_act, g, f, nullptr);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = gv[j][e];
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (k.post != PBT_NORM_NONE) u[j][e] = fmaf(u[j][e] * s1.y, g1[j][e], b1[j][e]);
-        o[j][e] = fmaf(k.beta * f[e], u[j][e], k.alpha * o[j][e]);
-      }
-      put8(row_at<R>(a.out, row) + c, o[j], n[j]);
+      for (int e = 0; e < 8; ++e) u[e] = fmaf(u[e] * s1.y, g1[e], b1[e]);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(k.beta * f[e], u[e], k.alpha * o[e]);
+    put8(row_at<R>(a.out, row) + c, o, n);
     if (k.pre != PBT_NORM_NONE) {
-      s2 = row_stats<T, J>(o, n, k.pre, d, k.eps, red, ph);
+      clear_past(o, n);
+      s2 = row_stats(o, n, k.pre, d, k.eps, sum);
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const int c = (l + T * j) * 8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[j][e] = fmaf(o[j][e] * s2.y, g2[j][e], b2[j][e]);
-        put8(row_at<A>(a.z, row) + c, o[j], n[j]);
-      }
+      for (int e = 0; e < 8; ++e) o[e] = fmaf(o[e] * s2.y, g2[e], b2[e]);
+      put8(row_at<A>(a.z, row) + c, o, n);
     }
     if (a.stats && l == 0) reinterpret_cast<float4*>(a.stats)[row] = make_float4(s1.x, s1.y, s2.x, s2.y);
   }
 }
 
-template <class A, class R, int T, int J>
-hipError_t launch(const BlockArgs& a, hipStream_t s) {
-  constexpr int GROUPS = block_threads(T) / T;
-  const int64_t most = 2048 / a.n.P + 1;   // slabs of a member: a few workgroups for every compute unit, all members together
-  int64_t slabs = (a.n.rows + GROUPS - 1) / GROUPS;
-  if (slabs > most) slabs = most;
-  const int64_t rows_per_slab = (a.n.rows + slabs - 1) / slabs;
-  hipLaunchKernelGGL((block_forward_kernel<A, R, T, J>), dim3((unsigned)slabs, a.n.P), dim3(block_threads(T)), 0, s, a, rows_per_slab);
-  return hipGetLastError();
-}
 template <class A, class R>
-hipError_t by_width(const BlockArgs& a, hipStream_t s) {
-  const BlockShape b = block_shape(a.n.d);
-  if (b.T == 16) return launch<A, R, 16, 1>(a, s);
-  if (b.T == 64) return b.J == 1 ? launch<A, R, 64, 1>(a, s) : launch<A, R, 64, 2>(a, s);
-  if (b.T == 256) return b.J == 1 ? launch<A, R, 256, 1>(a, s) : launch<A, R, 256, 2>(a, s);
-  return launch<A, R, 512, 2>(a, s);
+void launch(const BlockArgs& a, hipStream_t s) {
+  const BlockTeam t = block_team(a.n.d);
+  int extra = 0;
+  for (const float* p : {a.p.post_gain, a.p.post_bias, a.p.pre_gain, a.p.pre_bias, a.p.gate}) extra += p ? 4 : 0;
+  const int moved = (int)((a.n.pre != PBT_NORM_NONE ? 2 : 1) * sizeof(A) + (a.n.gate == PBT_GATE_ROWS ? sizeof(A) : 0) + 2 * sizeof(R));
+  const int64_t per_slab = slab_rows(a.n, extra, moved, std::max(16 / (t.threads / 64), 1));
+  const dim3 grid((unsigned)((a.n.rows + per_slab - 1) / per_slab), a.n.P), block(t.threads);
+  if (a.n.d < 8) hipLaunchKernelGGL((block_forward_kernel<A, R, 16, 256, true>), grid, block, 0, s, a, per_slab);
+  else if (t.T == 16) hipLaunchKernelGGL((block_forward_kernel<A, R, 16, 256, false>), grid, block, 0, s, a, per_slab);
+  else if (t.T == 64) hipLaunchKernelGGL((block_forward_kernel<A, R, 64, 256, false>), grid, block, 0, s, a, per_slab);
+  else if (t.threads <= 512) hipLaunchKernelGGL((block_forward_kernel<A, R, WIDE, 512, false>), grid, block, 0, s, a, per_slab);
+  else hipLaunchKernelGGL((block_forward_kernel<A, R, WIDE, 1024, false>), grid, block, 0, s, a, per_slab);
 }
 
 }  // namespace
 
 hipError_t block_norm_forward(const BlockArgs& a, hipStream_t s) {
   const bool act16 = a.n.dtype == PBT_DTYPE_BF16, res16 = a.n.res_dtype == PBT_DTYPE_BF16;
-  if (act16) return res16 ? by_width<bf16_t, bf16_t>(a, s) : by_width<bf16_t, float>(a, s);
-  return res16 ? by_width<float, bf16_t>(a, s) : by_width<float, float>(a, s);
+  if (act16) res16 ? launch<bf16_t, bf16_t>(a, s) : launch<bf16_t, float>(a, s);
+  else res16 ? launch<float, bf16_t>(a, s) : launch<float, float>(a, s);
+  return hipGetLastError();
 }
 
 }  // namespace pbt

@@ -22,10 +22,11 @@ __device__ __forceinline__ void stream16(void* p, const Vec16& v) {
 }
 constexpr int64_t LAST_CACHE = (int64_t)256 << 20;   // bytes of the cache in front of memory: what a call writes beyond it is not found there afterwards
 
-// elements 0 .. n-1 (n >= 8: all eight); those past n are zero
-template <class T> struct Raw8;   // eight elements as they lie in memory
+// Eight elements as they lie in memory, of which n exist (n >= 8: all; n <= 0: none).  load: one by one where n < 8.  load_end: where at least eight
+// elements end at p + n, the eight that do; get_end moves them to their places, away from the load, which is then one instruction that nothing waits for.
+template <class T> struct Raw8;
 template <> struct Raw8<bf16_t> {
-  Vec16 a;
+  Vec16 a{{0, 0, 0, 0}};
   __device__ __forceinline__ void load(const bf16_t* p, int n) {
     if (n >= 8) { a = load16(p); return; }
     a = Vec16{{0, 0, 0, 0}};
@@ -33,13 +34,16 @@ template <> struct Raw8<bf16_t> {
     for (int e = 0; e < 7; ++e)
       if (e < n) a.w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
   }
+  __device__ __forceinline__ void load_end(const bf16_t* p, int n) {
+    if (n > 0) a = load16(p + (n < 8 ? n - 8 : 0));
+  }
   __device__ __forceinline__ void get(float* v) const {
 #pragma unroll
     for (int q = 0; q < 4; ++q) { v[2 * q] = __uint_as_float(a.w[q] << 16); v[2 * q + 1] = __uint_as_float(a.w[q] & 0xffff0000u); }
   }
 };
 template <> struct Raw8<float> {
-  Vec16 a, b;
+  Vec16 a{{0, 0, 0, 0}}, b{{0, 0, 0, 0}};
   __device__ __forceinline__ void load(const float* p, int n) {
     if (n >= 8) { a = load16(p); b = load16(p + 4); return; }
     a = b = Vec16{{0, 0, 0, 0}};
@@ -47,11 +51,31 @@ template <> struct Raw8<float> {
     for (int e = 0; e < 7; ++e)
       if (e < n) (e < 4 ? a : b).w[e & 3] = __float_as_uint(p[e]);
   }
+  __device__ __forceinline__ void load_end(const float* p, int n) {
+    if (n > 0) {
+      p += n < 8 ? n - 8 : 0;
+      a = load16(p);
+      b = load16(p + 4);
+    }
+  }
   __device__ __forceinline__ void get(float* v) const {
 #pragma unroll
     for (int q = 0; q < 4; ++q) { v[q] = __uint_as_float(a.w[q]); v[4 + q] = __uint_as_float(b.w[q]); }
   }
 };
+template <class T>
+__device__ __forceinline__ void get_end(const Raw8<T>& r, float* v, int n) {
+  r.get(v);
+  if (n < 8 && n > 0) {
+    const int by = 8 - n;
+#pragma unroll
+    for (int step = 1; step < 8; step *= 2)
+      if (by & step) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e + step < 8 ? v[e + step] : 0.f;
+      }
+  }
+}
 __device__ __forceinline__ void put8(bf16_t* p, const float* v, int n) {
   const Vec16 o{{f2bf_pair(v[0], v[1]), f2bf_pair(v[2], v[3]), f2bf_pair(v[4], v[5]), f2bf_pair(v[6], v[7])}};
   if (n >= 8) { store16(p, o); return; }
