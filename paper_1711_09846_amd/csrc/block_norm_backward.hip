@@ -25,7 +25,8 @@ __device__ __forceinline__ void to_lds(float4* lds, int stride, int which, int l
   lds[(2 * which + 1) * stride + l] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-template <class A, class R, int T, int MOST, bool TINY>
+// ALL: every parameter's gradient; else those of the two gains only
+template <class A, class R, int T, int MOST, bool TINY, bool ALL>
 __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64_t rows_per_slab) {
   extern __shared__ float4 lds[];   // [PARAMS][2][threads of a team], then the team's sums
   constexpr int ROWS = T == WIDE ? 1 : 256 / T;
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
         s1 += t[e];
         s2 = fmaf(t[e], xh[e], s2);
         acc[2][e] = fmaf(dz[e], xh[e], acc[2][e]);
-        acc[3][e] += dz[e];
+        if (ALL) acc[3][e] += dz[e];
       }
     }
     if (r + ROWS < r_end) fetch(r + ROWS);   // (on its way while this row is reduced)
@@ -155,9 +156,9 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
       xh[e] = k.alpha * t[e];             // dx
       df[e] = k.beta * t[e] * df[e];      // dgate
       t[e] = k.beta * f[e] * t[e];        // v
-      acc[4][e] += df[e];
+      if (ALL) acc[4][e] += df[e];
       acc[0][e] = fmaf(t[e], yh[e], acc[0][e]);
-      acc[1][e] += t[e];
+      if (ALL) acc[1][e] += t[e];
     }
     put8(row_at<R>(a.dx, row) + c, xh, n);
     if (rows_gate) put8(row_at<A>(a.dgate, row) + c, df, n);
@@ -260,13 +261,13 @@ int64_t rows_per_slab(const pbt_block_norm& n) {
 int64_t slabs_of(const pbt_block_norm& n) { return (n.rows + rows_per_slab(n) - 1) / rows_per_slab(n); }
 
 // more than 64 KB of LDS need a permission, once on every device (wide teams have 72 to 128 KB, whose compute unit has no room for a second of them anyway)
-template <class A, class R, int MOST>
+template <class A, class R, int MOST, bool ALL>
 hipError_t launch_wide(const BlockArgs& a, int64_t per_slab, dim3 grid, dim3 block, size_t lds, hipStream_t s) {
   if (lds > 64 * 1024) {
-    const hipError_t e = allow_lds<&block_backward_kernel<A, R, WIDE, MOST, false>>(128 * 1024);
+    const hipError_t e = allow_lds<&block_backward_kernel<A, R, WIDE, MOST, false, ALL>>(128 * 1024);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((block_backward_kernel<A, R, WIDE, MOST, false>), grid, block, lds, s, a, per_slab);
+  hipLaunchKernelGGL((block_backward_kernel<A, R, WIDE, MOST, false, ALL>), grid, block, lds, s, a, per_slab);
   return hipGetLastError();
 }
 template <class A, class R>
@@ -275,12 +276,15 @@ hipError_t launch(const BlockArgs& a, int64_t slabs, hipStream_t s) {
   const int64_t per_slab = rows_per_slab(a.n);
   const dim3 grid((unsigned)slabs, a.n.P), block(t.threads);
   const size_t lds = (size_t)(t.T == WIDE ? PARAMS : SUMS) * 2 * (t.T == WIDE ? t.threads : t.T) * sizeof(float4);
-  if (a.n.d < 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, true>), grid, block, lds, s, a, per_slab);
-  else if (t.T == 16) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, false>), grid, block, lds, s, a, per_slab);
-  else if (t.T == 64) hipLaunchKernelGGL((block_backward_kernel<A, R, 64, 256, false>), grid, block, lds, s, a, per_slab);
-  else if (t.threads <= 512) return launch_wide<A, R, 512>(a, per_slab, grid, block, lds, s);
-  else if (t.threads <= 768) return launch_wide<A, R, 768>(a, per_slab, grid, block, lds, s);
-  else return launch_wide<A, R, 1024>(a, per_slab, grid, block, lds, s);
+  if (a.n.d < 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, true, true>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 16) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, false, true>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 64) hipLaunchKernelGGL((block_backward_kernel<A, R, 64, 256, false, true>), grid, block, lds, s, a, per_slab);
+  else if (t.threads <= 512) return launch_wide<A, R, 512, true>(a, per_slab, grid, block, lds, s);
+  else if (t.threads <= 768) return launch_wide<A, R, 768, true>(a, per_slab, grid, block, lds, s);
+  // (1024 threads have 128 registers each: with all five sums some go to memory.  2 x 2048 rows of 7000: 155 us with two sums, 282 with five; up to 768
+  // threads the number makes no difference)
+  else if (a.g.post_bias || a.g.pre_bias || a.g.gate) return launch_wide<A, R, 1024, true>(a, per_slab, grid, block, lds, s);
+  else return launch_wide<A, R, 1024, false>(a, per_slab, grid, block, lds, s);
   return hipGetLastError();
 }
 

@@ -550,3 +550,16 @@ def test_operators_on_another_stream_and_in_graphs():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, outs)), k
+
+
+@pytest.mark.parametrize("names", [("post_gain", "pre_gain"), ("post_gain",), ("pre_bias", "gate"), ()])
+def test_block_norm_some_parameters_of_wide_rows(names):
+    """Which parameters' gradients are asked for does not change the others, at a width whose backward kernel depends on it."""
+    P, rows, d = 2, 5, 6200
+    c = _case(P, rows, d, "layer", "layer", "vector", "none", "bf16", "fp32")
+    op = binding.BlockNorm(d, members=P, post="layer", pre="layer", gate="vector")
+    _, _, stats = op.forward(c["y"], c["x"], c["params"])
+    dy, dx, _, grads = op.backward(c["y"], c["x"], c["params"], stats, c["dout"], c["dz"])
+    some = {k: torch.full_like(grads[k], 9.0) for k in names}
+    dy2, dx2, _, _ = op.backward(c["y"], c["x"], c["params"], stats, c["dout"], c["dz"], grads=some)
+    assert torch.equal(dy, dy2) and torch.equal(dx, dx2) and all(torch.equal(some[k], grads[k]) for k in names)
