@@ -128,10 +128,10 @@ def lib():
         L.pbt_clip_gradients.argtypes = [C.POINTER(PbtGrad), i32, i32, vp, i64, vp, vp, sz, vp]
         L.pbt_rotary_plan.argtypes = [C.POINTER(PbtRotary), vp, sz, vp]
         L.pbt_rotary_apply.argtypes = [C.POINTER(PbtRotary), vp, C.POINTER(PbtHeads), i32, i32, i64, i32, vp, i32, i64, i64, i32, vp]
-        block, rows, params = C.POINTER(PbtBlockNorm), C.POINTER(PbtRows), C.POINTER(PbtBlockParams)
-        L.pbt_block_norm_forward.argtypes = [block, rows, rows, rows, params, rows, rows, vp, vp]
-        L.pbt_block_norm_work_bytes.argtypes = [block, C.POINTER(sz)]
-        L.pbt_block_norm_backward.argtypes = [block, rows, rows, rows, params, vp, rows, rows, rows, rows, rows, params, vp, sz, vp]
+        # (matrices and parameters, pbt_rows and pbt_block_params, by address: BlockNorm lays a call's side by side in one array)
+        L.pbt_block_norm_forward.argtypes = [C.POINTER(PbtBlockNorm), vp, vp, vp, vp, vp, vp, vp, vp]
+        L.pbt_block_norm_work_bytes.argtypes = [C.POINTER(PbtBlockNorm), C.POINTER(sz)]
+        L.pbt_block_norm_backward.argtypes = [C.POINTER(PbtBlockNorm), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         for name in EXPORTS:
             if name != "pbt_last_error":
                 getattr(L, name).restype = C.c_int
@@ -405,6 +405,7 @@ _LAYOUTS = {"half": 0, "interleaved": 1}
 _NORMS = {"none": 0, "layer": 1, "rms": 2}
 _GATES = {"none": 0, "vector": 1, "rows": 2}
 _GATE_ACTS = {"none": 0, "tanh": 4, "sigmoid": 5, "silu": 6}
+_I64x16, _I64x28 = C.c_int64 * 16, C.c_int64 * 28
 BLOCK_PARAMS = ("post_gain", "post_bias", "pre_gain", "pre_bias", "gate")
 
 
@@ -552,91 +553,119 @@ class BlockNorm:
         self.width, self.members = width, members
         self.settings = PbtBlockNorm(0, members, width, _choice(_NORMS, post, "post"), _choice(_NORMS, pre, "pre"), _choice(_GATES, gate, "gate"),
                                      _choice(_GATE_ACTS, act, "act"), 0, 0, eps, alpha, beta)
-        self._check(lib().pbt_block_norm_work_bytes(C.byref(self.settings), C.byref(C.c_size_t())))
+        self._pre, self._rows_gate = self.settings.pre != 0, self.settings.gate == 2
+        self._param_shapes = ((members, width), (width,)) if members == 1 else ((members, width),)
+        self._known = {}      # rows and types of a call -> its settings and the bytes its backward pass works in
+        self._query(self.settings)
 
     @staticmethod
-    def _check(rc):
+    def _query(settings):
+        n = C.c_size_t()
+        rc = lib().pbt_block_norm_work_bytes(C.byref(settings), C.byref(n))
         if rc != 0:
             raise PbtError(rc, lib().pbt_last_error(None).decode())
+        return n.value
 
     def _settings(self, y, x):
-        s = PbtBlockNorm.from_buffer_copy(self.settings)
-        if y.dim() != 2 or y.shape[1] != self.width or x.shape != y.shape or y.shape[0] % self.members:
-            raise ValueError("y and x: [members * rows, width]")
-        s.rows, s.dtype, s.res_dtype = y.shape[0] // self.members, _dtype_code(y), _dtype_code(x)
-        return s
+        shape = y.shape
+        key = (shape, y.dtype, x.dtype)
+        known = self._known.get(key)
+        if known is None:
+            if len(shape) != 2 or shape[1] != self.width or shape[0] % self.members:
+                raise ValueError("y and x: [members * rows, width]")
+            s = PbtBlockNorm.from_buffer_copy(self.settings)
+            s.rows, s.dtype, s.res_dtype = shape[0] // self.members, _dtype_code(y), _dtype_code(x)
+            if len(self._known) >= 256:      # (batches of ever new sizes)
+                self._known.clear()
+            known = self._known[key] = (s, self._query(s))
+        return known
 
     @staticmethod
     def _rows(t, like, what):
+        """(address, pitch) of a matrix."""
         if t is None:
-            return PbtRows(0, 0)
-        if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+            return 0, 0
+        if t.shape != like.shape or t.dtype is not like.dtype or t.device != like.device:
             raise ValueError("%s: shape, type and device of %s are wanted" % (what, tuple(like.shape)))
-        if t.shape[1] > 1 and t.stride(1) != 1:
+        (n, d), (pitch, step) = t.shape, t.stride()
+        if step != 1 and d > 1:
             raise ValueError("%s: a row's elements must be adjacent" % what)
-        return PbtRows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+        return t.data_ptr(), pitch if n > 1 else d
 
     def _params(self, params, device):
+        """The fields of pbt_block_params."""
         import torch
-        out, stride = PbtBlockParams(), None
-        for name, t in params.items():
-            if name not in BLOCK_PARAMS:
-                raise ValueError("unknown parameter %r" % name)
+        if not params:
+            return 0, 0, 0, 0, 0, self.width
+        out, stride, seen = [], None, 0
+        for name in BLOCK_PARAMS:
+            t = params.get(name)
             if t is None:
+                out.append(0)
+                seen += name in params
                 continue
-            if t.dtype != torch.float32 or t.device != device or t.shape[-1] != self.width or t.numel() != self.members * self.width:
+            seen += 1
+            if t.dtype is not torch.float32 or t.device != device or t.shape not in self._param_shapes:
                 raise ValueError("%s: float32 [members, width] on the tensors' device" % name)
-            if (self.width > 1 and t.stride(-1) != 1) or (self.members > 1 and t.dim() != 2):
-                raise ValueError("%s: float32 [members, width] with adjacent channels" % name)
-            s = t.stride(0) if self.members > 1 else self.width
-            if stride is not None and s != stride:
-                raise ValueError("parameters lie at different distances between members")
-            stride = s
-            setattr(out, name, t.data_ptr())
-        out.stride = self.width if stride is None else stride
+            steps = t.stride()
+            if steps[-1] != 1 and self.width > 1:
+                raise ValueError("%s: adjacent channels are wanted" % name)
+            if self.members > 1:
+                if stride is not None and steps[0] != stride:
+                    raise ValueError("parameters lie at different distances between members")
+                stride = steps[0]
+            out.append(t.data_ptr())
+        if seen != len(params):
+            raise ValueError("parameters are %s, not %s" % (", ".join(BLOCK_PARAMS), ", ".join(params)))
+        out.append(self.width if stride is None else stride)
         return out
 
     def forward(self, y, x, params=None, gate=None, out=None, z=None, stats=True):
         """Returns (out, z, stats); z is None with pre = "none", stats (float32 [rows, 4], for backward) with stats = False."""
         import torch
-        s = self._settings(y, x)
+        s, _ = self._settings(y, x)
+        device = y.device
+        if device.type != "cuda" or x.device != device or x.shape != y.shape:
+            raise ValueError("y and x: device tensors of one shape, on one device")
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if z is None and s.pre:
-            z = torch.empty(y.shape, dtype=y.dtype, device=y.device)
-        st = torch.empty((y.shape[0], 4), dtype=torch.float32, device=y.device) if stats else None
-        like_x = x if x.device == y.device else y
-        p = self._params(params or {}, y.device)
-        _call(_on_device((y, x)), lib().pbt_block_norm_forward, C.byref(s), C.byref(self._rows(y, y, "y")), C.byref(self._rows(x, like_x, "x")),
-              C.byref(self._rows(gate, y, "gate")), C.byref(p), C.byref(self._rows(out, x, "out")), C.byref(self._rows(z if s.pre else None, y, "z")),
-              0 if st is None else st.data_ptr())
-        return out, (z if s.pre else None), st
+            out = torch.empty_like(x)
+        if not self._pre:
+            z = None
+        elif z is None:
+            z = torch.empty_like(y)
+        st = torch.empty((y.shape[0], 4), dtype=torch.float32, device=device) if stats else None
+        a = _I64x16(*self._rows(y, y, "y"), *self._rows(x, x, "x"), *self._rows(gate if self._rows_gate else None, y, "gate"), *self._rows(out, x, "out"),
+                    *self._rows(z, y, "z"), *self._params(params, device))
+        at = C.addressof(a)
+        _call(device, lib().pbt_block_norm_forward, C.byref(s), at, at + 16, at + 32, at + 80, at + 48, at + 64, 0 if st is None else st.data_ptr())
+        return out, z, st
 
     def backward(self, y, x, params, stats, dout, dz, gate=None, dy=None, dx=None, dgate=None, grads=None):
         """Gradients from those of out and z (either may be None: zero).  Returns (dy, dx, dgate, grads): dgate is None unless gate = "rows";
         grads: dict of float32 [members, width] for the parameters in params (or the tensors given as `grads`, which are overwritten)."""
         import torch
-        s = self._settings(y, x)
-        if stats.shape != (y.shape[0], 4) or stats.dtype != torch.float32 or not stats.is_contiguous() or stats.device != y.device:
+        s, work_bytes = self._settings(y, x)
+        device = y.device
+        if device.type != "cuda" or x.device != device or x.shape != y.shape:
+            raise ValueError("y and x: device tensors of one shape, on one device")
+        if stats.shape != (y.shape[0], 4) or stats.dtype is not torch.float32 or not stats.is_contiguous() or stats.device != device:
             raise ValueError("stats: what forward returned")
-        params = params or {}
         if dy is None:
-            dy = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+            dy = torch.empty_like(y)
         if dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        rows_gate = s.gate == 2
-        if rows_gate and dgate is None:
-            dgate = torch.empty(y.shape, dtype=y.dtype, device=y.device)
+            dx = torch.empty_like(x)
+        if not self._rows_gate:
+            gate = dgate = None
+        elif dgate is None:
+            dgate = torch.empty_like(y)
         if grads is None:
-            names = [k for k, t in params.items() if t is not None]
-            flat = torch.empty((len(names), self.members, self.width), dtype=torch.float32, device=y.device)
-            grads = dict(zip(names, flat))
-        p, g = self._params(params, y.device), self._params(grads, y.device)
-        n = C.c_size_t()
-        self._check(lib().pbt_block_norm_work_bytes(C.byref(s), C.byref(n)))
-        work = torch.empty(n.value, dtype=torch.uint8, device=y.device)   # (of this call: calls on two streams do not meet in it)
-        _call(_on_device((y, x)), lib().pbt_block_norm_backward, C.byref(s), C.byref(self._rows(y, y, "y")), C.byref(self._rows(x, x, "x")),
-              C.byref(self._rows(gate, y, "gate")), C.byref(p), stats.data_ptr(), C.byref(self._rows(dout, x, "dout")), C.byref(self._rows(dz, y, "dz")),
-              C.byref(self._rows(dy, y, "dy")), C.byref(self._rows(dx, x, "dx")), C.byref(self._rows(dgate if rows_gate else None, y, "dgate")), C.byref(g),
-              work.data_ptr(), n.value)
-        return dy, dx, (dgate if rows_gate else None), grads
+            names = [k for k, t in (params or {}).items() if t is not None]
+            grads = dict(zip(names, torch.empty((len(names), self.members, self.width), dtype=torch.float32, device=device).unbind(0)))
+        a = _I64x28(*self._rows(y, y, "y"), *self._rows(x, x, "x"), *self._rows(gate, y, "gate"), *self._rows(dout, x, "dout"),
+                    *self._rows(dz if self._pre else None, y, "dz"), *self._rows(dy, y, "dy"), *self._rows(dx, x, "dx"), *self._rows(dgate, y, "dgate"),
+                    *self._params(params, device), *self._params(grads, device))
+        at = C.addressof(a)
+        work = torch.empty(work_bytes, dtype=torch.uint8, device=device)   # (of this call: calls on two streams do not meet in it)
+        _call(device, lib().pbt_block_norm_backward, C.byref(s), at, at + 16, at + 32, at + 128, stats.data_ptr(), at + 48, at + 64, at + 80, at + 96, at + 112, at + 176,
+              work.data_ptr(), work_bytes)
+        return dy, dx, dgate, grads
