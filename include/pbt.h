@@ -72,7 +72,10 @@ enum { PBT_DTYPE_FP32 = 0, PBT_DTYPE_BF16 = 1 };      /* BF16 = bf16 operands, f
 enum { PBT_ROLE_LR = 0, PBT_ROLE_BETA1 = 1, PBT_ROLE_WD = 2, /* meaning of a hyperparameter column */
        PBT_ROLE_LR_G = 3, PBT_ROLE_LR_D = 4,                  /* GAN: generator / discriminator learning rate */
        PBT_ROLE_ENTROPY_COST = 5,                             /* actor-critic: weight of the entropy bonus */
-       PBT_ROLE_DROPOUT = 6, PBT_ROLE_LABEL_SMOOTH = 7 };     /* transformer: dropout rate, label smoothing */
+       PBT_ROLE_DROPOUT = 6, PBT_ROLE_LABEL_SMOOTH = 7,       /* transformer: dropout rate, label smoothing */
+       PBT_ROLE_CLIP_NORM = 8 };                              /* bf16 compute, optimiser as a pass of its own (fuse_optimizer 0), not GAN: the
+                                                                 largest norm of the member's gradient.  The update uses g * clip / norm where the norm over
+                                                                 all parameters is larger (as pbt_clip_gradients; PBT_ARR_GRAD keeps the gradient as it was) */
 
 /* Arrays of the population store that pbt_get_state / pbt_set_state address. */
 enum {
@@ -96,7 +99,8 @@ enum {
   PBT_ARR_TRAJ_OBS = 13,
   PBT_ARR_TRAJ_ACT = 14,
   PBT_ARR_TRAJ_REW = 15,
-  PBT_ARR_COUNT = 16
+  PBT_ARR_GRAD_NORM = 16, /* float [P]        norm of the last step's gradient before clipping (with a PBT_ROLE_CLIP_NORM column only) */
+  PBT_ARR_COUNT = 17
 };
 
 typedef struct {
@@ -182,7 +186,7 @@ typedef struct {
   int64_t b_off[PBT_MAX_DIMS];      /* start of b_l */
   /* every parameter array in order of appearance (dense workloads: W_0, b_0, W_1, ...; transformer:
      token embedding [V][d], position embedding [S][d], per block {ln1 gain, ln1 bias, Wqkv [d][3d],
-     bqkv, Wo [d][d], bo, ln2 gain, ln2 bias, W1 [d][f], b1, W2 [f][d], b2}, final gain, final bias,
+     bqkv, Wo [d][d], bo, ln2 gain, ln2 bias, W1 [d][f], b1, W2 [f][d], b2, with pbt_tf_options.block_norm four more}, final gain, final bias,
      Whead [d][V], bhead) */
   int32_t n_seg;
   int64_t seg_off[PBT_MAX_SEGMENTS];
@@ -201,6 +205,41 @@ pbt_status pbt_query_sizes(const pbt_config* cfg, size_t* state_bytes, size_t* s
  * failure *out is NULL.  The two buffers must outlive the handle. */
 pbt_status pbt_init(const pbt_config* cfg, void* d_state, size_t state_bytes, void* d_scratch, size_t scratch_bytes,
                     void* hip_stream, pbt_handle** out);
+
+/* Rotary positions, see pbt_rotary_apply for what the fields mean; kinds of norms, see pbt_block_norm_forward. */
+enum { PBT_ROTARY_HALF = 0, PBT_ROTARY_INTERLEAVED = 1 };
+enum { PBT_ROTARY_SCALE_NONE = 0, PBT_ROTARY_SCALE_LINEAR = 1, PBT_ROTARY_SCALE_BASE = 2, PBT_ROTARY_SCALE_RAMP = 3 };
+typedef struct {
+  int32_t rot_dim;                  /* even, 2..PBT_ROTARY_MAX_DIM */
+  int32_t layout, scaling;          /* PBT_ROTARY_*, PBT_ROTARY_SCALE_* */
+  int32_t unused;                   /* 0 */
+  double base;                      /* > 0, finite */
+  double factor;                    /* > 0, finite (LINEAR, BASE, RAMP) */
+  double trained_len, low, high;    /* RAMP: trained_len > 0, low < high */
+  double gain;                      /* finite; multiplies the rotated part */
+} pbt_rotary;
+#define PBT_ROTARY_MAX_DIM 512
+enum { PBT_NORM_NONE = 0, PBT_NORM_LAYER = 1, PBT_NORM_RMS = 2 };
+
+/* Options of the transformer workload beyond pbt_config (PBT_WL_TRANSFORMER only), and pbt_query_sizes / pbt_init with them; opts = NULL is the same as the
+ * calls without.
+ *   rotary             1: query and key heads are turned by their positions 0 .. tf_seq - 1 between the joint projection and attention, settings in
+ *                      `rot` (rot_dim at most the head width), see pbt_rotary_apply.
+ *   learned_positions  0: the position table is neither added to the embeddings nor updated (it stays in the layout).
+ *   block_norm         PBT_NORM_LAYER or PBT_NORM_RMS: a norm with gain and a learned gate per channel after each branch, in place of the plain residual sum,
+ *                        h <- alpha h + beta gate * N(drop(branch(LN(h)))),
+ *                      see pbt_block_norm_forward.  Every block has four more parameter arrays behind W2 and b2: gain and gate of the attention
+ *                      branch, gain and gate of the feed-forward branch ([d] each, initially 1), so that at most 5 blocks fit PBT_MAX_SEGMENTS; tf_d_model <= 2048.
+ *                      PBT_NORM_NONE: the plain sum; alpha and beta are then 1. */
+typedef struct {
+  int32_t rotary, learned_positions, block_norm;
+  float alpha, beta;
+  int32_t unused;                   /* 0 */
+  pbt_rotary rot;
+} pbt_tf_options;
+pbt_status pbt_query_sizes_tf(const pbt_config* cfg, const pbt_tf_options* opts, size_t* state_bytes, size_t* scratch_bytes, pbt_layout* layout);
+pbt_status pbt_init_tf(const pbt_config* cfg, const pbt_tf_options* opts, void* d_state, size_t state_bytes, void* d_scratch, size_t scratch_bytes,
+                       void* hip_stream, pbt_handle** out);
 
 /* A prior over one hyperparameter column: uniform on [lo, hi] or log-uniform (exp of a uniform
  * draw on [ln lo, ln hi]; needs 0 < lo). */
@@ -364,18 +403,7 @@ pbt_status pbt_clip_gradients(const pbt_grad* h_grads, int32_t n_grads, int32_t 
  *   RAMP    f_j (w + (1 - w) / factor), w = (trained_len f_j / (2 pi) - low) / (high - low) clamped to [0, 1]: pairs that turn often within
  *           the trained length keep their pace, those that turn less than `low` times are slowed by `factor`.
  * Angles are formed in double from 32- or 64-bit positions and reduced before they are rounded. */
-enum { PBT_ROTARY_HALF = 0, PBT_ROTARY_INTERLEAVED = 1 };
-enum { PBT_ROTARY_SCALE_NONE = 0, PBT_ROTARY_SCALE_LINEAR = 1, PBT_ROTARY_SCALE_BASE = 2, PBT_ROTARY_SCALE_RAMP = 3 };
-typedef struct {
-  int32_t rot_dim;                  /* even, 2..PBT_ROTARY_MAX_DIM */
-  int32_t layout, scaling;          /* PBT_ROTARY_*, PBT_ROTARY_SCALE_* */
-  int32_t unused;                   /* 0 */
-  double base;                      /* > 0, finite */
-  double factor;                    /* > 0, finite (LINEAR, BASE, RAMP) */
-  double trained_len, low, high;    /* RAMP: trained_len > 0, low < high */
-  double gain;                      /* finite; multiplies the rotated part */
-} pbt_rotary;
-#define PBT_ROTARY_MAX_DIM 512
+/* (pbt_rotary: declared with pbt_tf_options above) */
 /* Writes the table of frequencies, rot_dim / 2 doubles (in turns per position), that pbt_rotary_apply reads; d_table is 8-byte aligned. */
 pbt_status pbt_rotary_plan(const pbt_rotary* r, void* d_table, size_t table_bytes, void* hip_stream);
 /* One group of heads: element (row, head, e) at d_src[row * src_row + head * src_head + e].  dst is src with the same strides (in
@@ -402,7 +430,6 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
  * NONE.  gate: NONE (factor 1), VECTOR (one of the parameters: a factor per channel, the same for all rows of a member) or ROWS (a matrix); a is
  * gate_act, PBT_ACT_NONE, SIGMOID, SILU or TANH.  y, z, the gate's matrix and their gradients are of `dtype`, x, out and theirs
  * of `res_dtype`; parameters and their gradients are float.  z is formed from out before it is rounded. */
-enum { PBT_NORM_NONE = 0, PBT_NORM_LAYER = 1, PBT_NORM_RMS = 2 };
 enum { PBT_GATE_NONE = 0, PBT_GATE_VECTOR = 1, PBT_GATE_ROWS = 2 };
 #define PBT_BLOCK_NORM_MAX_D 8192
 typedef struct {

@@ -26,7 +26,7 @@ import numpy as np
 
 from . import nets, optim, philox, pbt
 
-ROLE_LR, ROLE_ENTROPY_COST = 0, 5
+ROLE_LR, ROLE_ENTROPY_COST, ROLE_CLIP_NORM = 0, 5, 8
 HIST = 10
 
 
@@ -100,7 +100,10 @@ def update_on_batch(spec, m, obs, actions, rewards):
     loss, grads = loss_and_grads(spec, m, obs, actions, rewards)
     lr = m.h[spec.roles.index(ROLE_LR)]
     m.t += 1
-    for j, g in enumerate([a for gr in grads for a in gr]):
+    grads = [a for gr in grads for a in gr]
+    if ROLE_CLIP_NORM in spec.roles:
+        grads = optim.clip(grads, m.h[spec.roles.index(ROLE_CLIP_NORM)])
+    for j, g in enumerate(grads):
         m.theta[j], m.opt["s0"][j] = optim.rmsprop(m.theta[j], g, m.opt["s0"][j], lr, spec.rho, spec.rms_eps)
     # float32 like the population store keeps it
     m.hist = (m.hist + [np.float32(np.asarray(rewards, dtype=np.float64).sum(axis=1).mean())])[-HIST:]

@@ -13,7 +13,7 @@ from . import nets, optim, philox, pbt
 
 OPT_SGD_MOMENTUM, OPT_ADAM, OPT_RMSPROP = 0, 1, 2
 # hyperparameter roles (what a column of h means)
-ROLE_LR, ROLE_BETA1, ROLE_WD = 0, 1, 2
+ROLE_LR, ROLE_BETA1, ROLE_WD, ROLE_CLIP_NORM = 0, 1, 2, 8
 
 
 class ClassifierSpec:
@@ -59,6 +59,8 @@ def apply_optimizer(spec, member, flat_grads):
     """theta <- update(theta, g, state | h) for every parameter array."""
     lr = hyper(spec, member, ROLE_LR, None)
     member.t += 1
+    if ROLE_CLIP_NORM in spec.roles:
+        flat_grads = optim.clip(flat_grads, hyper(spec, member, ROLE_CLIP_NORM, None))
     for j, g in enumerate(flat_grads):
         th = member.theta[j]
         if spec.optimizer == OPT_SGD_MOMENTUM:

@@ -19,6 +19,12 @@ Each function updates one parameter array and returns the new arrays.
 import numpy as np
 
 
+def clip(grads, max_norm):
+    """The member's gradient arrays, scaled down to max_norm where their common norm is larger."""
+    norm = np.sqrt(sum((g * g).sum() for g in grads))
+    return [g * (max(float(max_norm), 0.0) / norm) for g in grads] if norm > float(max_norm) else grads
+
+
 def sgd_momentum(theta, g, v, lr, mu):
     v = mu * v + g
     theta = theta - float(lr) * v

@@ -18,6 +18,9 @@ token sequences:
            cross-entropy of the next token (target = (1-e) onehot + e/V);
            one Adam update with the member's learning rate; p and e are the
            member's second and third hyperparameters.
+           Options: query and key heads turned by rotary positions before their scores; no learned positions; a norm with a gate per channel
+           that closes every branch, h <- alpha h + beta gate N(drop(...)) (operators.py).  A clip-norm hyperparameter scales the gradient
+           down to that norm before the update.
   eval     minus the perplexity exp(mean cross-entropy) of the next token on
            held-out sequences, without dropout or smoothing.
 
@@ -40,20 +43,35 @@ read q(W).
 """
 import numpy as np
 
-from . import nets, optim, philox, pbt
+from . import nets, operators, optim, philox, pbt
 
-ROLE_LR, ROLE_DROPOUT, ROLE_LABEL_SMOOTH = 0, 6, 7
+ROLE_LR, ROLE_DROPOUT, ROLE_LABEL_SMOOTH, ROLE_CLIP_NORM = 0, 6, 7, 8
 LN_EPS = 1e-5
 
 
 class TransformerSpec:
     def __init__(self, vocab, d_model, n_heads, d_ff, n_layers, seq, batch, seed,
-                 roles=(ROLE_LR, ROLE_DROPOUT, ROLE_LABEL_SMOOTH), beta1=0.9, beta2=0.999, eps=1e-8, bf16_storage=False):
+                 roles=(ROLE_LR, ROLE_DROPOUT, ROLE_LABEL_SMOOTH), beta1=0.9, beta2=0.999, eps=1e-8, bf16_storage=False, rotary=None,
+                 learned_positions=True, block_norm="none", alpha=1.0, beta=1.0):
         assert d_model % n_heads == 0
         self.V, self.d, self.H, self.f, self.L, self.S, self.B = vocab, d_model, n_heads, d_ff, n_layers, seq, batch
         self.seed, self.roles = seed, list(roles)
         self.beta1, self.beta2, self.eps = beta1, beta2, eps
         self.q = nets.round_bf16 if bf16_storage else nets.identity
+        # rotary: dict(rot_dim, and any of base, layout, scaling, factor, trained, low, high, gain) or None; block_norm: kind of the norm after a branch
+        self.learned_positions = learned_positions
+        self.rotary = None
+        if rotary:
+            kw = dict(rotary)
+            self.rotary = dict(layout=kw.pop("layout", "half"), gain=kw.pop("gain", 1.0), freq=operators.rotary_frequencies(kw.pop("rot_dim"), **kw))
+        self.norm = None if block_norm == "none" else operators.BlockNorm(block_norm, "layer", "vector", "none", LN_EPS, alpha, beta)
+
+    def turn(self, heads, backward=False):
+        """Heads [B][H][S][dh] at positions 0 .. S-1."""
+        B, H, S, dh = heads.shape
+        rows = heads.transpose(0, 2, 1, 3).reshape(B * S, H, dh)
+        out = operators.rotary(rows, np.arange(B * S) % S, self.rotary["freq"], self.rotary["layout"], self.rotary["gain"], backward)
+        return out.reshape(B, S, H, dh).transpose(0, 2, 1, 3)
 
     def param_shapes(self):
         """Names and shapes of the parameter arrays, in the order of the flat parameter vector."""
@@ -63,6 +81,8 @@ class TransformerSpec:
             out += [("ln1_g%d" % l, (d,)), ("ln1_b%d" % l, (d,)), ("wqkv%d" % l, (d, 3 * d)), ("bqkv%d" % l, (3 * d,)),
                     ("wo%d" % l, (d, d)), ("bo%d" % l, (d,)), ("ln2_g%d" % l, (d,)), ("ln2_b%d" % l, (d,)),
                     ("w1%d" % l, (d, f)), ("b1%d" % l, (f,)), ("w2%d" % l, (f, d)), ("b2%d" % l, (d,))]
+            if self.norm:
+                out += [("post1_g%d" % l, (d,)), ("gate1_g%d" % l, (d,)), ("post2_g%d" % l, (d,)), ("gate2_g%d" % l, (d,))]
         out += [("lnf_g", (d,)), ("lnf_b", (d,)), ("whead", (d, V)), ("bhead", (V,))]
         return out
 
@@ -141,6 +161,27 @@ class _Drop:
         return keep.reshape(shape) * self.scale
 
 
+def _close_params(spec, P, l, k):
+    """Parameters of the norm that closes branch k of block l: its own gain and gate, gain and bias of the LayerNorm that follows; with their names."""
+    after = ("ln2_g%d" % l, "ln2_b%d" % l) if k == 1 else ("lnf_g", "lnf_b") if l + 1 == spec.L else ("ln1_g%d" % (l + 1), "ln1_b%d" % (l + 1))
+    names = dict(post_gain="post%d_g%d" % (k, l), gate="gate%d_g%d" % (k, l), pre_gain=after[0], pre_bias=after[1])
+    return {a: P[b] for a, b in names.items()}, names
+
+
+def _close(spec, P, l, k, y, h):
+    """(stream after branch k of block l, the LayerNorm of it, cache); the LayerNorm sees the stream before it is rounded."""
+    out, z, cache = spec.norm.forward(y, h, _close_params(spec, P, l, k)[0])
+    return spec.q(out), z, cache
+
+
+def _close_backward(spec, P, l, k, cache, dout, dz, G):
+    """(gradient of the branch's output, of the stream before it); parameters' gradients into G."""
+    dy, dx, _, grads = spec.norm.backward(cache, dout, dz)
+    for a, name in _close_params(spec, P, l, k)[1].items():
+        G[name] = grads[a]
+    return spec.q(dy), spec.q(dx)
+
+
 def forward(spec, P, tokens, drop):
     """tokens [B][S] ints.  Returns (logits [B*S][V], cache)."""
     q = spec.q
@@ -149,15 +190,18 @@ def forward(spec, P, tokens, drop):
     dh = d // H
     n = B * S
     c = {"tokens": tokens}
-    h = q(q(P["tok_emb"])[tokens] + q(P["pos_emb"])[None, :S, :]).reshape(n, d)
+    h = q(q(P["tok_emb"])[tokens] + (q(P["pos_emb"])[None, :S, :] if spec.learned_positions else 0.0)).reshape(n, d)
     c["layers"] = []
     for l in range(spec.L):
         lc = {"h_in": h}
-        y, lc["ln1"] = layernorm(h, P["ln1_g%d" % l], P["ln1_b%d" % l])
-        u = q(y)
+        if spec.norm is None or l == 0:
+            y, lc["ln1"] = layernorm(h, P["ln1_g%d" % l], P["ln1_b%d" % l])
+        u = q(y)      # (with block norms a block's first LayerNorm comes out of the norm that closes the block before it)
         qkv = q(u @ q(P["wqkv%d" % l]) + P["bqkv%d" % l])
         heads = qkv.reshape(B, S, 3, H, dh).transpose(2, 0, 3, 1, 4)          # [3][B][H][S][dh]
         qh, kh, vh = heads[0], heads[1], heads[2]
+        if spec.rotary:
+            qh, kh = q(spec.turn(qh)), q(spec.turn(kh))
         s = q(qh @ kh.transpose(0, 1, 3, 2))                                  # raw scores, stored
         p = causal_softmax(s * (1.0 / np.sqrt(dh)))
         m0 = drop.mask(4 * l + 0, p.shape)
@@ -165,9 +209,13 @@ def forward(spec, P, tokens, drop):
         o = q(pd @ vh).transpose(0, 2, 1, 3).reshape(n, d)
         a = q(o @ q(P["wo%d" % l]) + P["bo%d" % l])
         m1 = drop.mask(4 * l + 1, a.shape)
-        h = q(h + a * m1)
+        if spec.norm:
+            h, y, lc["bn1"] = _close(spec, P, l, 1, q(a * m1), h)
+        else:
+            h = q(h + a * m1)
         lc.update(u=u, qh=qh, kh=kh, vh=vh, pq=pq, pd=pd, m0=m0, o=o, m1=m1, h_mid=h)
-        y, lc["ln2"] = layernorm(h, P["ln2_g%d" % l], P["ln2_b%d" % l])
+        if spec.norm is None:
+            y, lc["ln2"] = layernorm(h, P["ln2_g%d" % l], P["ln2_b%d" % l])
         u2 = q(y)
         f = u2 @ q(P["w1%d" % l]) + P["b1%d" % l]
         z1, r = q(f), q(np.maximum(f, 0.0))
@@ -175,10 +223,14 @@ def forward(spec, P, tokens, drop):
         fd = q(r * m2)
         g = q(fd @ q(P["w2%d" % l]) + P["b2%d" % l])
         m3 = drop.mask(4 * l + 3, g.shape)
-        h = q(h + g * m3)
+        if spec.norm:
+            h, y, lc["bn2"] = _close(spec, P, l, 2, q(g * m3), h)
+        else:
+            h = q(h + g * m3)
         lc.update(u2=u2, z1=z1, fd=fd, m2=m2, m3=m3)
         c["layers"].append(lc)
-    y, c["lnf"] = layernorm(h, P["lnf_g"], P["lnf_b"])
+    if spec.norm is None:
+        y, c["lnf"] = layernorm(h, P["lnf_g"], P["lnf_b"])
     uf = q(y)
     c["uf"] = uf
     logits = uf @ q(P["whead"]) + P["bhead"]
@@ -197,21 +249,27 @@ def backward(spec, P, cache, dlogits):
     dl = q(dlogits)
     G["whead"], G["bhead"] = cache["uf"].T @ dl, dl.sum(axis=0)
     du = q(dl @ q(P["whead"]).T)
-    dx, G["lnf_g"], G["lnf_b"] = layernorm_backward(du, P["lnf_g"], cache["lnf"])
-    dhid = q(dx)
+    if spec.norm:
+        dbranch, dhid = _close_backward(spec, P, spec.L - 1, 2, cache["layers"][-1]["bn2"], None, du, G)
+    else:
+        dx, G["lnf_g"], G["lnf_b"] = layernorm_backward(du, P["lnf_g"], cache["lnf"])
+        dbranch = dhid = q(dx)
     for l in range(spec.L - 1, -1, -1):
         lc = cache["layers"][l]
         # feed-forward branch
-        dg = q(dhid * lc["m3"])
+        dg = q(dbranch * lc["m3"])
         G["w2%d" % l], G["b2%d" % l] = lc["fd"].T @ dg, dg.sum(axis=0)
         dfd = q(dg @ q(P["w2%d" % l]).T)
         dz1 = q(dfd * lc["m2"] * (lc["z1"] > 0.0))
         G["w1%d" % l], G["b1%d" % l] = lc["u2"].T @ dz1, dz1.sum(axis=0)
         du2 = q(dz1 @ q(P["w1%d" % l]).T)
-        dx, G["ln2_g%d" % l], G["ln2_b%d" % l] = layernorm_backward(du2, P["ln2_g%d" % l], lc["ln2"])
-        dhid = q(dhid + dx)
+        if spec.norm:
+            dbranch, dhid = _close_backward(spec, P, l, 1, lc["bn1"], dhid, du2, G)
+        else:
+            dx, G["ln2_g%d" % l], G["ln2_b%d" % l] = layernorm_backward(du2, P["ln2_g%d" % l], lc["ln2"])
+            dbranch = dhid = q(dhid + dx)
         # attention branch
-        da = q(dhid * lc["m1"])
+        da = q(dbranch * lc["m1"])
         G["wo%d" % l], G["bo%d" % l] = lc["o"].T @ da, da.sum(axis=0)
         do = q(da @ q(P["wo%d" % l]).T).reshape(B, S, H, dh).transpose(0, 2, 1, 3)      # [B][H][S][dh]
         dv = q(lc["pd"].transpose(0, 1, 3, 2) @ do)
@@ -220,14 +278,20 @@ def backward(spec, P, cache, dlogits):
         ds = q(lc["pq"] * (dp - (dp * lc["pq"]).sum(axis=-1, keepdims=True)) * (1.0 / np.sqrt(dh)))
         dq = q(ds @ lc["kh"])
         dk = q(ds.transpose(0, 1, 3, 2) @ lc["qh"])
+        if spec.rotary:
+            dq, dk = q(spec.turn(dq, backward=True)), q(spec.turn(dk, backward=True))
         dqkv = np.stack([dq, dk, dv]).transpose(1, 3, 0, 2, 4).reshape(n, 3 * d)       # [B][S][3][H][dh]
         G["wqkv%d" % l], G["bqkv%d" % l] = lc["u"].T @ dqkv, dqkv.sum(axis=0)
         duu = q(dqkv @ q(P["wqkv%d" % l]).T)
+        if spec.norm and l > 0:
+            dbranch, dhid = _close_backward(spec, P, l - 1, 2, cache["layers"][l - 1]["bn2"], dhid, duu, G)
+            continue
         dx, G["ln1_g%d" % l], G["ln1_b%d" % l] = layernorm_backward(duu, P["ln1_g%d" % l], lc["ln1"])
-        dhid = q(dhid + dx)
+        dbranch = dhid = q(dhid + dx)
     dh0 = dhid.reshape(B, S, d)
     G["pos_emb"] = np.zeros_like(P["pos_emb"])
-    G["pos_emb"][:S] = dh0.sum(axis=0)
+    if spec.learned_positions:
+        G["pos_emb"][:S] = dh0.sum(axis=0)
     G["tok_emb"] = np.zeros_like(P["tok_emb"])
     np.add.at(G["tok_emb"], tokens.reshape(-1), dh0.reshape(n, d))
     return G
@@ -254,10 +318,13 @@ def step(spec, m, i, s, pool, want_grads=False):
     loss, grads = loss_and_grads(spec, m, pool[idx], s, i)
     lr = m.h[spec.roles.index(ROLE_LR)]
     m.t += 1
+    raw = grads
+    if ROLE_CLIP_NORM in spec.roles:
+        grads = optim.clip(grads, m.h[spec.roles.index(ROLE_CLIP_NORM)])
     for j, g in enumerate(grads):
         m.theta[j], m.opt["s0"][j], m.opt["s1"][j] = optim.adam(
             m.theta[j], g, m.opt["s0"][j], m.opt["s1"][j], m.t, lr, spec.beta1, spec.beta2, spec.eps, 0.0)
-    return (loss, grads) if want_grads else loss
+    return (loss, raw) if want_grads else loss
 
 
 def evaluate(spec, m, eval_seqs, chunk=64):

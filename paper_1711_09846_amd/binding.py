@@ -16,17 +16,18 @@ LIB_PATH = os.path.join(_HERE, "libpbt.so")
 
 PBT_MAX_DIMS, PBT_MAX_HYPER, PBT_MAX_SEGMENTS = 16, 8, 96
 (ARR_W32, ARR_OPT0, ARR_OPT1, ARR_W16, ARR_GRAD, ARR_HYPER, ARR_SCORE, ARR_LOSS, ARR_T, ARR_ORDER, ARR_DONOR,
- ARR_PARENT, ARR_HIST, ARR_TRAJ_OBS, ARR_TRAJ_ACT, ARR_TRAJ_REW) = range(16)
+ ARR_PARENT, ARR_HIST, ARR_TRAJ_OBS, ARR_TRAJ_ACT, ARR_TRAJ_REW, ARR_GRAD_NORM) = range(17)
 _ARR_DTYPE = {ARR_W32: np.float32, ARR_OPT0: np.float32, ARR_OPT1: np.float32, ARR_W16: np.uint16,
               ARR_GRAD: np.float32, ARR_HYPER: np.float32, ARR_SCORE: np.float32, ARR_LOSS: np.float32,
               ARR_T: np.int32, ARR_ORDER: np.int32, ARR_DONOR: np.int32, ARR_PARENT: np.int32, ARR_HIST: np.float32,
-              ARR_TRAJ_OBS: np.uint16, ARR_TRAJ_ACT: np.int32, ARR_TRAJ_REW: np.float32}
+              ARR_TRAJ_OBS: np.uint16, ARR_TRAJ_ACT: np.int32, ARR_TRAJ_REW: np.float32, ARR_GRAD_NORM: np.float32}
 
 EXPORTS = ["pbt_query_sizes", "pbt_init", "pbt_step", "pbt_eval", "pbt_exploit_explore", "pbt_get_state",
            "pbt_set_state", "pbt_state_ptr", "pbt_destroy", "pbt_last_error", "pbt_batched_gemm_bf16",
            "pbt_timing_enable", "pbt_timing_stride", "pbt_timing_read", "pbt_init_population", "pbt_set_priors",
            "pbt_step_static", "pbt_timing_enable_classes", "pbt_timing_read_class", "pbt_clip_work_bytes", "pbt_clip_gradients",
-           "pbt_rotary_plan", "pbt_rotary_apply", "pbt_block_norm_forward", "pbt_block_norm_work_bytes", "pbt_block_norm_backward"]
+           "pbt_rotary_plan", "pbt_rotary_apply", "pbt_block_norm_forward", "pbt_block_norm_work_bytes", "pbt_block_norm_backward",
+           "pbt_query_sizes_tf", "pbt_init_tf"]
 STATIC_SCRATCH_BYTES = 8 << 20
 (K_NONE, K_FETCH, K_GEMM_FWD, K_HEAD, K_GEMM_WGRAD, K_GEMM_DGRAD, K_BIAS_GRAD, K_OPTIMIZER, K_RANK, K_COPY,
  K_FUSED_STEP) = range(-1, 10)
@@ -68,6 +69,11 @@ class PbtRotary(C.Structure):
                 ("factor", C.c_double), ("trained_len", C.c_double), ("low", C.c_double), ("high", C.c_double), ("gain", C.c_double)]
 
 
+class PbtTfOptions(C.Structure):
+    _fields_ = [("rotary", C.c_int32), ("learned_positions", C.c_int32), ("block_norm", C.c_int32), ("alpha", C.c_float), ("beta", C.c_float),
+                ("unused", C.c_int32), ("rot", PbtRotary)]
+
+
 class PbtHeads(C.Structure):
     _fields_ = [("d_src", C.c_void_p), ("d_dst", C.c_void_p), ("src_row", C.c_int64), ("src_head", C.c_int64), ("dst_row", C.c_int64),
                 ("dst_head", C.c_int64), ("heads", C.c_int32), ("unused", C.c_int32)]
@@ -106,6 +112,8 @@ def lib():
         vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
         L.pbt_query_sizes.argtypes = [C.POINTER(PbtConfig), C.POINTER(sz), C.POINTER(sz), C.POINTER(PbtLayout)]
         L.pbt_init.argtypes = [C.POINTER(PbtConfig), vp, sz, vp, sz, vp, C.POINTER(vp)]
+        L.pbt_query_sizes_tf.argtypes = [C.POINTER(PbtConfig), C.POINTER(PbtTfOptions), C.POINTER(sz), C.POINTER(sz), C.POINTER(PbtLayout)]
+        L.pbt_init_tf.argtypes = [C.POINTER(PbtConfig), C.POINTER(PbtTfOptions), vp, sz, vp, sz, vp, C.POINTER(vp)]
         L.pbt_step.argtypes = [vp, C.POINTER(vp), i32, i64, i32, vp]
         L.pbt_step_static.argtypes = [vp, C.POINTER(vp), i32, i64, i32, vp]
         L.pbt_eval.argtypes = [vp, C.POINTER(vp), i32, vp]
@@ -192,9 +200,23 @@ def make_config(wl, seed, P=None, n_trunc=None, eval_chunk=0, fuse_optimizer=0):
     return c
 
 
-def query_sizes(cfg):
+def make_tf_options(wl):
+    """PbtTfOptions from a workload description's tf_options (a dict with any of rotary: the keyword arguments of Rotary, rot_dim among them,
+    learned_positions, block_norm: "layer" or "rms", alpha, beta), or None."""
+    opts = getattr(wl, "tf_options", None)
+    if not opts:
+        return None
+    o = PbtTfOptions(0, int(opts.get("learned_positions", True)), _choice(_NORMS, opts.get("block_norm", "none"), "block_norm"),
+                     opts.get("alpha", 1.0), opts.get("beta", 1.0), 0)
+    if opts.get("rotary"):
+        o.rotary, o.rot = 1, rotary_settings(**opts["rotary"])
+    return o
+
+
+def query_sizes(cfg, tf_options=None):
     st, sc, lay = C.c_size_t(), C.c_size_t(), PbtLayout()
-    rc = lib().pbt_query_sizes(C.byref(cfg), C.byref(st), C.byref(sc), C.byref(lay))
+    opts = None if tf_options is None else C.byref(tf_options)
+    rc = lib().pbt_query_sizes_tf(C.byref(cfg), opts, C.byref(st), C.byref(sc), C.byref(lay))
     if rc != 0:
         raise PbtError(rc, lib().pbt_last_error(None).decode())
     return st.value, sc.value, lay
@@ -238,17 +260,18 @@ def unpack_params(lay, dims, flat):
 class Population:
     """Owns the device buffers (through torch) and a library handle."""
 
-    def __init__(self, cfg, device="cuda:0"):
+    def __init__(self, cfg, device="cuda:0", tf_options=None):
         import torch
         self.torch = torch
         self.cfg = cfg
+        self.tf_options = tf_options
         self.device = torch.device(device)
-        state_bytes, scratch_bytes, self.layout = query_sizes(cfg)
+        state_bytes, scratch_bytes, self.layout = query_sizes(cfg, tf_options)
         self.state = torch.empty(state_bytes, dtype=torch.uint8, device=self.device)
         self.scratch = torch.empty(scratch_bytes, dtype=torch.uint8, device=self.device)
         self._h = C.c_void_p()
         with torch.cuda.device(self.device):
-            rc = lib().pbt_init(C.byref(cfg), self.state.data_ptr(), state_bytes, self.scratch.data_ptr(),
+            rc = lib().pbt_init_tf(C.byref(cfg), None if tf_options is None else C.byref(tf_options), self.state.data_ptr(), state_bytes, self.scratch.data_ptr(),
                                 scratch_bytes, self._stream(), C.byref(self._h))
         if rc != 0:
             raise PbtError(rc, lib().pbt_last_error(None).decode())
@@ -495,6 +518,11 @@ class GradClip:
         return norms
 
 
+def rotary_settings(rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained=0.0, low=1.0, high=32.0, gain=1.0):
+    """PbtRotary from names."""
+    return PbtRotary(rot_dim, _choice(_LAYOUTS, layout, "layout"), _choice(_SCALINGS, scaling, "scaling"), 0, base, factor, trained, low, high, gain)
+
+
 class Rotary:
     """Rotary positions on heads (pbt_rotary_plan, pbt_rotary_apply): rot_dim, base, layout ("half", "interleaved"), scaling ("none",
     "linear", "base", "ramp" with factor, and for "ramp" trained, low, high) and gain as in include/pbt.h.  Making one writes the table of frequencies and
@@ -502,7 +530,7 @@ class Rotary:
 
     def __init__(self, rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained=0.0, low=1.0, high=32.0, gain=1.0, device="cuda:0"):
         import torch
-        self.settings = PbtRotary(rot_dim, _choice(_LAYOUTS, layout, "layout"), _choice(_SCALINGS, scaling, "scaling"), 0, base, factor, trained, low, high, gain)
+        self.settings = rotary_settings(rot_dim, base, layout, scaling, factor, trained, low, high, gain)
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())

@@ -268,6 +268,7 @@ static pbt_status a2c_update(pbt_handle* h, hipStream_t s) {
   const bool fused = c.fuse_optimizer != 0;
   if ((st = backward(h, net, L - 1, R, A, Z, dZ, true, fused ? &oa : nullptr, nullptr, nullptr, 0, s)) != PBT_OK) return st;
   if (fused) return optimizer_rest(h, oa, 0, L, L - 1, S, s);
+  if ((st = clip_step(h, &oa, s)) != PBT_OK) return st;
   PBT_LAUNCH(h, PBT_K_OPTIMIZER, s, optimizer_step(oa, s));
   return PBT_OK;
 }

@@ -1,6 +1,7 @@
 // C ABI of the population step: configuration checks, carving of the caller's device buffers,
 // and the kernel sequences behind pbt_step / pbt_eval / pbt_exploit_explore.
 #include "dense_host.h"
+#include "operators.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -52,6 +53,16 @@ pbt_status fail(pbt_handle* h, pbt_status code, const char* fmt, ...) {
   g_last_error = buf;
   return code;
 }
+
+pbt_status clip_step(pbt_handle* h, OptArgs* oa, hipStream_t s) {
+  const Plan& p = h->plan;
+  if (p.col_clip < 0) return PBT_OK;
+  float* factor = h->sc<float>(p.o_gfactor);
+  PBT_LAUNCH(h, PBT_K_OPTIMIZER, s, grad_factor(h->sc<float>(p.o_grad), p.lay.stride, h->cfg.P, h->st<float>(p.o_hyper) + p.col_clip, h->cfg.n_hyper,
+                                                h->st<float>(p.o_gnorm), factor, h->sc<void>(p.o_gwork), s));
+  oa->g_scale = factor;
+  return PBT_OK;
+}
 }  // namespace pbt
 
 namespace {
@@ -88,7 +99,7 @@ pbt_status check_config(const pbt_config* c, Plan* pl) {
   if (!gan && !tf && c->dims[c->n_layers] > 32) return fail(nullptr, PBT_EUNSUPPORTED, "more than 32 outputs in the last layer");
   pl->a2c.col_ent = -1;
   pl->tf.col_drop = pl->tf.col_ls = -1;
-  pl->col_lr = pl->col_beta1 = pl->col_wd = -1;
+  pl->col_lr = pl->col_beta1 = pl->col_wd = pl->col_clip = -1;
   pl->gan.col_lr_g = pl->gan.col_lr_d = -1;
   for (int k = 0; k < c->n_hyper; ++k) {
     if (c->hyper_role[k] == PBT_ROLE_LR) pl->col_lr = k;
@@ -99,8 +110,14 @@ pbt_status check_config(const pbt_config* c, Plan* pl) {
     else if (c->hyper_role[k] == PBT_ROLE_ENTROPY_COST) pl->a2c.col_ent = k;
     else if (c->hyper_role[k] == PBT_ROLE_DROPOUT) pl->tf.col_drop = k;
     else if (c->hyper_role[k] == PBT_ROLE_LABEL_SMOOTH) pl->tf.col_ls = k;
+    else if (c->hyper_role[k] == PBT_ROLE_CLIP_NORM) pl->col_clip = k;
     else return fail(nullptr, PBT_EINVAL, "unknown hyper_role[%d] = %d", k, c->hyper_role[k]);
     if (std::isnan(c->hyper_max[k])) return fail(nullptr, PBT_EINVAL, "hyper_max[%d] is NaN", k);
+  }
+  if (pl->col_clip >= 0) {
+    if (gan) return fail(nullptr, PBT_EUNSUPPORTED, "a clip-norm column is not built for the GAN workload, whose two networks are updated one after the other");
+    if (c->compute_dtype != PBT_DTYPE_BF16) return fail(nullptr, PBT_EUNSUPPORTED, "a clip-norm column needs bf16 compute: fp32 steps keep their gradients on the chip");
+    if (c->fuse_optimizer) return fail(nullptr, PBT_EUNSUPPORTED, "a clip-norm column needs fuse_optimizer = 0: the whole gradient has to be there before the update");
   }
   if (gan) {
     if (pl->gan.col_lr_g < 0 || pl->gan.col_lr_d < 0) return fail(nullptr, PBT_EINVAL, "the GAN workload needs a generator and a discriminator learning-rate column");
@@ -122,9 +139,15 @@ pbt_status check_config(const pbt_config* c, Plan* pl) {
   return PBT_OK;
 }
 
-pbt_status make_plan(const pbt_config* c, Plan* pl) {
+pbt_status make_plan(const pbt_config* c, const pbt_tf_options* opts, Plan* pl) {
   pbt_status st = check_config(c, pl);
   if (st != PBT_OK) return st;
+  std::memset(&pl->tf.opt, 0, sizeof pl->tf.opt);
+  pl->tf.opt.learned_positions = 1;
+  if (opts) {
+    if ((st = tf_check_options(c, opts)) != PBT_OK) return st;
+    pl->tf.opt = *opts;
+  }
   const int L = c->n_layers;
   const int64_t P = c->P, B = c->batch;
   const bool gan = c->workload == PBT_WL_GAN;
@@ -179,10 +202,14 @@ pbt_status make_plan(const pbt_config* c, Plan* pl) {
   pl->o_recip = s.take(P * 4);
   pl->o_nrecip = s.take(4);
   pl->o_hist = c->workload == PBT_WL_A2C ? s.take(P * 12 * 4) : 0;
+  pl->o_gnorm = pl->col_clip >= 0 ? s.take(P * 4) : 0;
+  pl->tf.o_turns = pl->tf.opt.rotary ? s.take(PBT_ROTARY_MAX_DIM / 2 * sizeof(double)) : 0;
   pl->state_bytes = s.off;
 
   Carver w;
   pl->o_grad = w.take(pw * 4);
+  pl->o_gfactor = pl->col_clip >= 0 ? w.take(P * 4) : 0;
+  pl->o_gwork = pl->col_clip >= 0 ? w.take(grad_factor_work_bytes(lay.stride, (int)P)) : 0;
   // (every workload carves what its step uses first and sets step_scratch_bytes; the held-out pass's and the exploit pass's buffers follow)
   pl->fused_small = false;
   pl->eval_chunk = 0;
@@ -295,6 +322,9 @@ pbt_status arr_info(pbt_handle* h, int which, ArrInfo* ai) {
       else if (which == PBT_ARR_TRAJ_ACT) *ai = {p.a2c.o_act, 4, (int64_t)c.batch * c.unroll, true};
       else *ai = {p.a2c.o_rew, 4, (int64_t)c.batch * c.unroll, true};
       return PBT_OK;
+    case PBT_ARR_GRAD_NORM:
+      if (p.col_clip < 0) return fail(h, PBT_EINVAL, "GRAD_NORM exists only with a clip-norm column");
+      *ai = {p.o_gnorm, 4, 1, false}; return PBT_OK;
     default: return fail(h, PBT_EINVAL, "unknown array id %d", which);
   }
 }
@@ -384,6 +414,8 @@ pbt_status step_bf16(pbt_handle* h, const float* train_x, const int32_t* train_y
       PBT_LAUNCH(h, PBT_K_GEMM_WGRAD, s, gemm_store_f32(wg, G + p.lay.w_off[l], N, S, s));
   }
   if (fused) return optimizer_rest(h, oa, 0, L, L - 1, S, s);
+  const pbt_status cst = clip_step(h, &oa, s);
+  if (cst != PBT_OK) return cst;
   PBT_LAUNCH(h, PBT_K_OPTIMIZER, s, optimizer_step(oa, s));
   return PBT_OK;
 }
@@ -425,8 +457,12 @@ static hipError_t reset_store(pbt_handle* h, hipStream_t s);
 extern "C" {
 
 pbt_status pbt_query_sizes(const pbt_config* cfg, size_t* state_bytes, size_t* scratch_bytes, pbt_layout* layout) {
+  return pbt_query_sizes_tf(cfg, nullptr, state_bytes, scratch_bytes, layout);
+}
+
+pbt_status pbt_query_sizes_tf(const pbt_config* cfg, const pbt_tf_options* opts, size_t* state_bytes, size_t* scratch_bytes, pbt_layout* layout) {
   Plan pl;
-  pbt_status st = make_plan(cfg, &pl);
+  pbt_status st = make_plan(cfg, opts, &pl);
   if (st != PBT_OK) return st;
   if (state_bytes) *state_bytes = pl.state_bytes;
   if (scratch_bytes) *scratch_bytes = pl.scratch_bytes;
@@ -436,10 +472,15 @@ pbt_status pbt_query_sizes(const pbt_config* cfg, size_t* state_bytes, size_t* s
 
 pbt_status pbt_init(const pbt_config* cfg, void* d_state, size_t state_bytes, void* d_scratch, size_t scratch_bytes,
                     void* hip_stream, pbt_handle** out) {
+  return pbt_init_tf(cfg, nullptr, d_state, state_bytes, d_scratch, scratch_bytes, hip_stream, out);
+}
+
+pbt_status pbt_init_tf(const pbt_config* cfg, const pbt_tf_options* opts, void* d_state, size_t state_bytes, void* d_scratch, size_t scratch_bytes,
+                       void* hip_stream, pbt_handle** out) {
   if (!out) return fail(nullptr, PBT_EINVAL, "out is NULL");
   *out = nullptr;
   Plan pl;
-  pbt_status st = make_plan(cfg, &pl);
+  pbt_status st = make_plan(cfg, opts, &pl);
   if (st != PBT_OK) return st;
   if (!d_state || !d_scratch) return fail(nullptr, PBT_EINVAL, "device buffers must not be NULL");
   if (((uintptr_t)d_state | (uintptr_t)d_scratch) % BUF_ALIGN) return fail(nullptr, PBT_EINVAL, "device buffers must be 256-byte aligned");
@@ -474,6 +515,11 @@ static hipError_t reset_store(pbt_handle* h, hipStream_t s) {
   if (e == hipSuccess) e = fill_u32(h->st<uint32_t>(pl.o_donor), 0xffffffffu, P, s);  // -1
   if (e == hipSuccess) e = iota_i32(h->st<int32_t>(pl.o_parent), P, s);
   if (e == hipSuccess) e = iota_i32(h->st<int32_t>(pl.o_order), P, s);
+  if (e == hipSuccess && pl.tf.opt.rotary) {
+    RotaryFrequencies f;
+    rotary_frequencies(pl.tf.opt.rot, &f);
+    e = rotary_plan(f, pl.tf.opt.rot.rot_dim / 2, h->st<double>(pl.tf.o_turns), s);
+  }
   return e;
 }
 
@@ -527,8 +573,10 @@ pbt_status pbt_init_population(pbt_handle* h, const pbt_prior* priors, void* hip
     // embeddings and matrices uniform in +-1/sqrt(fan_in) (fan_in = d_model for the two tables), LayerNorm gains 1, every bias 0
     const int d = c.tf_d_model, f = c.tf_d_ff;
     a.seg_fan[0] = a.seg_fan[1] = d;
+    const bool normed = p.tf.opt.block_norm != PBT_NORM_NONE;
     for (int l = 0; l < c.n_layers; ++l) {
-      const int b0 = 2 + 12 * l;
+      const int b0 = 2 + (normed ? 16 : 12) * l;
+      for (int k = 12; k < 16 && normed; ++k) a.seg_const[b0 + k] = 1.f;
       a.seg_const[b0 + 0] = 1.f; a.seg_fan[b0 + 2] = d; a.seg_fan[b0 + 4] = d;
       a.seg_const[b0 + 6] = 1.f; a.seg_fan[b0 + 8] = d; a.seg_fan[b0 + 10] = f;
     }
@@ -740,7 +788,7 @@ pbt_status pbt_get_state(pbt_handle* h, int32_t which, int32_t member, void* h_d
 
 pbt_status pbt_set_state(pbt_handle* h, int32_t which, int32_t member, const void* h_src, size_t src_bytes,
                          void* hip_stream) {
-  if (which == PBT_ARR_GRAD || which == PBT_ARR_ORDER || which == PBT_ARR_DONOR || which == PBT_ARR_LOSS ||
+  if (which == PBT_ARR_GRAD || which == PBT_ARR_ORDER || which == PBT_ARR_DONOR || which == PBT_ARR_LOSS || which == PBT_ARR_GRAD_NORM ||
       which == PBT_ARR_TRAJ_OBS || which == PBT_ARR_TRAJ_ACT || which == PBT_ARR_TRAJ_REW)
     return fail(h, PBT_EINVAL, "array %d is an output and cannot be set", which);
   return xfer(h, which, member, const_cast<void*>(h_src), src_bytes, hip_stream, false);

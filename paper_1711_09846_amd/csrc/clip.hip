@@ -267,6 +267,20 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, int64_t pe
   walk<true, NT>(t, words, i, lo, hi, c);
 }
 
+// norm and factor of a member from its ranges' sums
+__global__ __launch_bounds__(256) void clip_factor_kernel(const double* __restrict__ part, int64_t n_part, const float* __restrict__ max_norm, int64_t max_norm_stride,
+                                                          float* __restrict__ norm, float* __restrict__ out) {
+  __shared__ double red[4];
+  const int i = blockIdx.x;
+  double s = 0.0;
+  for (int64_t k = threadIdx.x; k < n_part; k += 256) s += part[i * n_part + k];
+  const double n = sqrt(block_sum<256>(s, red));
+  if (threadIdx.x == 0) {
+    norm[i] = (float)n;
+    out[i] = factor(n, max_norm + i * max_norm_stride);
+  }
+}
+
 int64_t units(const pbt_grad& g) { return (g.len + 7) / 8; }
 int64_t units_of(const pbt_grad* g, int k0, int n) {
   int64_t total = 0;
@@ -319,6 +333,21 @@ ClipTable table(const pbt_grad* g, int k0, int n, bool* in_place) {
 }  // namespace
 
 size_t clip_work_bytes(const pbt_grad* g, int n, int P) { return (size_t)P * parts(g, n, P) * sizeof(double); }
+
+size_t grad_factor_work_bytes(int64_t stride, int P) {
+  const pbt_grad g{nullptr, nullptr, stride, stride, stride, PBT_DTYPE_FP32, 0};
+  return (size_t)P * parts(&g, 1, P) * sizeof(double);
+}
+hipError_t grad_factor(const float* G, int64_t stride, int P, const float* max_norm, int64_t max_norm_stride, float* norm, float* out, void* work, hipStream_t s) {
+  const pbt_grad g{G, nullptr, stride, stride, stride, PBT_DTYPE_FP32, 0};
+  bool in_place;
+  const ClipTable t = table(&g, 0, 1, &in_place);
+  const int64_t total = t.start[1], ranges = sum_ranges(total, P), per_range = (total + ranges - 1) / ranges;
+  double* part = static_cast<double*>(work);
+  hipLaunchKernelGGL(clip_sum_kernel, dim3((unsigned)ranges, P), dim3(256), 0, s, t, per_range, part, ranges, (int64_t)0);
+  hipLaunchKernelGGL(clip_factor_kernel, dim3(P), dim3(256), 0, s, part, ranges, max_norm, max_norm_stride, norm, out);
+  return hipGetLastError();
+}
 
 hipError_t clip_gradients(const pbt_grad* g, int n, int P, const float* max_norm, int64_t max_norm_stride, float* norm, void* work, hipStream_t s) {
   bool in_place;

@@ -52,15 +52,18 @@ struct A2CPlan {
   bool packed_in_grad;        // its packed weights lie over the gradients, which are cleared again before the update
 };
 
-struct TfBlockOff { int64_t ln1g, ln1b, wqkv, bqkv, wo, bo, ln2g, ln2b, w1, b1, w2, b2; };
+struct TfBlockOff { int64_t ln1g, ln1b, wqkv, bqkv, wo, bo, ln2g, ln2b, w1, b1, w2, b2, post[2], gate[2]; };   // post, gate: with block norms, of the attention and the feed-forward branch
 struct TfPlan {
   int col_drop, col_ls;
+  pbt_tf_options opt;
+  size_t o_turns;                               // the rotary frequencies (in d_state)
   int64_t tok, pos, lnfg, lnfb, whead, bhead;   // parameter offsets (elements)
   TfBlockOff blk[PBT_MAX_DIMS];
   // scratch offsets (bytes); activations are [P][batch*seq][width]
   size_t o_tokens, o_targets, o_h[PBT_MAX_DIMS + 1], o_hmid[PBT_MAX_DIMS];
   size_t o_mean1[PBT_MAX_DIMS], o_rstd1[PBT_MAX_DIMS], o_mean2[PBT_MAX_DIMS], o_rstd2[PBT_MAX_DIMS], o_meanf, o_rstdf;
   size_t o_u[PBT_MAX_DIMS], o_qkv[PBT_MAX_DIMS], o_pq[PBT_MAX_DIMS], o_pd[PBT_MAX_DIMS], o_o[PBT_MAX_DIMS];
+  size_t o_y[PBT_MAX_DIMS][2], o_bnstats[PBT_MAX_DIMS][2], o_bnwork;   // block norms: the branches' outputs, row statistics
   size_t o_u2[PBT_MAX_DIMS], o_z1[PBT_MAX_DIMS], o_fd[PBT_MAX_DIMS];
   size_t o_mask[PBT_MAX_DIMS][3];   // keep bits of the block's three dropout sites outside attention
   bool fused_attn;                  // one attention kernel per pass: no score / probability arrays, o_keep instead
@@ -85,6 +88,9 @@ struct Plan {
   int eval_chunk;
   bool fused_small;  // fp32: the whole step runs in one LDS-resident kernel
   int col_lr, col_beta1, col_wd;
+  int col_clip;              // largest gradient norm, or -1
+  size_t o_gnorm;            // (d_state) norms of the last gradients
+  size_t o_gfactor, o_gwork; // (d_scratch) the gradients' factors, partial sums
   GanPlan gan;
   A2CPlan a2c;
   TfPlan tf;
@@ -137,6 +143,12 @@ pbt_status fail(pbt_handle* h, pbt_status code, const char* fmt, ...);
     }                                                                                           \
   } while (0)
 
+// operators_abi.hip
+pbt_status check_rotary(const pbt_rotary* r);
+
+// abi.hip: with a clip-norm column, the gradients' norms and the factors that the optimiser multiplies them by (oa->g_scale)
+pbt_status clip_step(pbt_handle* h, OptArgs* oa, hipStream_t s);
+
 // gan_host.hip: the GAN workload (Section 4.3.1)
 pbt_status gan_check_and_plan(const pbt_config* c, Plan* pl, Carver* scratch);
 pbt_status gan_step(pbt_handle* h, const float* train_x, uint32_t step, hipStream_t s);
@@ -150,6 +162,7 @@ pbt_status a2c_step_on_policy(pbt_handle* h, const A2CEnv& env, uint32_t step, h
 pbt_status a2c_eval(pbt_handle* h, hipStream_t s);
 
 // transformer_host.hip: the language-model workload (Section 4.2.1)
+pbt_status tf_check_options(const pbt_config* c, const pbt_tf_options* o);
 pbt_status tf_layout(const pbt_config* c, Plan* pl);
 pbt_status tf_check_and_plan(const pbt_config* c, Plan* pl, Carver* scratch);
 pbt_status tf_step(pbt_handle* h, const int32_t* pool, uint32_t step, hipStream_t s);

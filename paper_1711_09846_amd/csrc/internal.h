@@ -119,6 +119,7 @@ struct OptArgs {
   int64_t xbegin[3] = {0, 0, 0}, xcount[3] = {0, 0, 0};
   // Adam's bias correction counts t[i] * t_mul + t_add updates (a network updated several times per step)
   int t_mul = 1, t_add = 0;
+  const float* g_scale = nullptr;   // factor of every member's gradient (clipping), or null
 };
 constexpr int OPT_MAX_RANGES = 4;
 hipError_t optimizer_step(const OptArgs& a, hipStream_t s);

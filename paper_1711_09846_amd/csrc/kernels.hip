@@ -145,7 +145,11 @@ __global__ __launch_bounds__(256) void optimizer_kernel(OptArgs a) {
     if (v >= nvec) break;
     const int64_t o = (int64_t)i * a.stride + begin + v * 4;
     float4 w = stream_load(a.W32 + o);
-    const float4 g = stream_load(a.G + o);
+    float4 g = stream_load(a.G + o);
+    if (a.g_scale) {
+      const float c = a.g_scale[i];
+      g = make_float4(g.x * c, g.y * c, g.z * c, g.w * c);
+    }
     float4 s0 = stream_load(a.S0 + o);
     float4 s1 = make_float4(0.f, 0.f, 0.f, 0.f);
     if (OPT == OPT_ADAM) s1 = stream_load(a.S1 + o);

@@ -98,9 +98,15 @@ __device__ __forceinline__ void put8(float* p, const float* v, int n) {
 size_t clip_work_bytes(const pbt_grad* g, int n, int P);
 hipError_t clip_gradients(const pbt_grad* g, int n, int P, const float* max_norm, int64_t max_norm_stride, float* norm, void* work, hipStream_t s);
 
+// The norm of G[P][stride] (all of it: padding is zero) and the factor that brings it down to max_norm[i * max_norm_stride]: norm[P], factor[P].
+size_t grad_factor_work_bytes(int64_t stride, int P);
+hipError_t grad_factor(const float* G, int64_t stride, int P, const float* max_norm, int64_t max_norm_stride, float* norm, float* factor, void* work, hipStream_t s);
+
 // ---- rotary.hip ----
 struct RotaryFrequencies { double turns[PBT_ROTARY_MAX_DIM / 2]; };
 hipError_t rotary_plan(const RotaryFrequencies& f, int n, double* table, hipStream_t s);
+// turns per position of every pair
+void rotary_frequencies(const pbt_rotary& r, RotaryFrequencies* f);
 struct RotaryArgs {
   pbt_heads g[4];
   int n_groups, heads;      // heads of all groups

@@ -7,6 +7,23 @@
 
 using namespace pbt;
 
+namespace pbt {
+pbt_status check_rotary(const pbt_rotary* r) {
+  if (!r) return fail(nullptr, PBT_EINVAL, "rotary settings are NULL");
+  if (r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > PBT_ROTARY_MAX_DIM) return fail(nullptr, PBT_EINVAL, "rot_dim = %d: even, 2..%d", r->rot_dim, PBT_ROTARY_MAX_DIM);
+  if (r->layout != PBT_ROTARY_HALF && r->layout != PBT_ROTARY_INTERLEAVED) return fail(nullptr, PBT_EINVAL, "unknown rotary layout %d", r->layout);
+  if (r->scaling < PBT_ROTARY_SCALE_NONE || r->scaling > PBT_ROTARY_SCALE_RAMP) return fail(nullptr, PBT_EINVAL, "unknown rotary scaling %d", r->scaling);
+  if (r->unused != 0) return fail(nullptr, PBT_EINVAL, "the unused field must be 0");
+  if (!(r->base > 0.0) || !std::isfinite(r->base)) return fail(nullptr, PBT_EINVAL, "base must be positive and finite");
+  if (!std::isfinite(r->gain)) return fail(nullptr, PBT_EINVAL, "gain must be finite");
+  if (r->scaling != PBT_ROTARY_SCALE_NONE && (!(r->factor > 0.0) || !std::isfinite(r->factor))) return fail(nullptr, PBT_EINVAL, "factor must be positive and finite");
+  if (r->scaling == PBT_ROTARY_SCALE_RAMP &&
+      (!(r->trained_len > 0.0) || !std::isfinite(r->trained_len) || !(r->low < r->high) || !std::isfinite(r->low) || !std::isfinite(r->high)))
+    return fail(nullptr, PBT_EINVAL, "ramp scaling needs trained_len > 0 and low < high, finite");
+  return PBT_OK;
+}
+}  // namespace pbt
+
 namespace {
 
 size_t elem_bytes(int dtype) { return dtype == PBT_DTYPE_BF16 ? 2 : 4; }
@@ -49,21 +66,6 @@ pbt_status check_grads(const pbt_grad* g, int n, int P, bool clip) {
       }
     }
   }
-  return PBT_OK;
-}
-
-pbt_status check_rotary(const pbt_rotary* r) {
-  if (!r) return fail(nullptr, PBT_EINVAL, "rotary settings are NULL");
-  if (r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > PBT_ROTARY_MAX_DIM) return fail(nullptr, PBT_EINVAL, "rot_dim = %d: even, 2..%d", r->rot_dim, PBT_ROTARY_MAX_DIM);
-  if (r->layout != PBT_ROTARY_HALF && r->layout != PBT_ROTARY_INTERLEAVED) return fail(nullptr, PBT_EINVAL, "unknown rotary layout %d", r->layout);
-  if (r->scaling < PBT_ROTARY_SCALE_NONE || r->scaling > PBT_ROTARY_SCALE_RAMP) return fail(nullptr, PBT_EINVAL, "unknown rotary scaling %d", r->scaling);
-  if (r->unused != 0) return fail(nullptr, PBT_EINVAL, "the unused field must be 0");
-  if (!(r->base > 0.0) || !std::isfinite(r->base)) return fail(nullptr, PBT_EINVAL, "base must be positive and finite");
-  if (!std::isfinite(r->gain)) return fail(nullptr, PBT_EINVAL, "gain must be finite");
-  if (r->scaling != PBT_ROTARY_SCALE_NONE && (!(r->factor > 0.0) || !std::isfinite(r->factor))) return fail(nullptr, PBT_EINVAL, "factor must be positive and finite");
-  if (r->scaling == PBT_ROTARY_SCALE_RAMP &&
-      (!(r->trained_len > 0.0) || !std::isfinite(r->trained_len) || !(r->low < r->high) || !std::isfinite(r->low) || !std::isfinite(r->high)))
-    return fail(nullptr, PBT_EINVAL, "ramp scaling needs trained_len > 0 and low < high, finite");
   return PBT_OK;
 }
 
@@ -161,18 +163,7 @@ pbt_status pbt_rotary_plan(const pbt_rotary* r, void* d_table, size_t table_byte
   const int pairs = r->rot_dim / 2;
   if (table_bytes < pairs * sizeof(double)) return fail(nullptr, PBT_ENOMEM, "table: %zu bytes given, %zu needed", table_bytes, pairs * sizeof(double));
   RotaryFrequencies f;
-  std::memset(&f, 0, sizeof f);
-  const double two_pi = 6.283185307179586476925;
-  const double base = r->scaling == PBT_ROTARY_SCALE_BASE && r->rot_dim > 2 ? r->base * std::pow(r->factor, r->rot_dim / (r->rot_dim - 2.0)) : r->base;
-  for (int j = 0; j < pairs; ++j) {
-    double w = std::pow(base, -2.0 * j / r->rot_dim);   // radians a position
-    if (r->scaling == PBT_ROTARY_SCALE_LINEAR) w /= r->factor;
-    if (r->scaling == PBT_ROTARY_SCALE_RAMP) {
-      const double at = (r->trained_len * w / two_pi - r->low) / (r->high - r->low), keep = at < 0.0 ? 0.0 : at > 1.0 ? 1.0 : at;
-      w *= keep + (1.0 - keep) / r->factor;
-    }
-    f.turns[j] = w / two_pi;
-  }
+  rotary_frequencies(*r, &f);
   const hipError_t e = rotary_plan(f, pairs, static_cast<double*>(d_table), static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return fail(nullptr, PBT_EDEVICE, "writing the rotary table failed: %s", hipGetErrorString(e));
   return PBT_OK;

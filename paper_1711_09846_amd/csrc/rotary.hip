@@ -4,6 +4,7 @@
 // much as moving a pair takes at the memory's rate, so a workgroup forms them once for a few rows, in LDS, and all heads of those rows use them.  A unit of
 // work is one 16-byte access of adjacent pairs (two where a pair's halves lie apart).
 #include <algorithm>
+#include <cmath>
 
 #include "operators.h"
 
@@ -243,6 +244,22 @@ hipError_t launch(RotaryArgs a, hipStream_t s) {
 }
 
 }  // namespace
+
+void rotary_frequencies(const pbt_rotary& r, RotaryFrequencies* f) {
+  const double two_pi = 6.283185307179586476925;
+  const double base = r.scaling == PBT_ROTARY_SCALE_BASE && r.rot_dim > 2 ? r.base * std::pow(r.factor, r.rot_dim / (r.rot_dim - 2.0)) : r.base;
+  for (int j = 0; j < PBT_ROTARY_MAX_DIM / 2; ++j) {
+    f->turns[j] = 0.0;
+    if (j >= r.rot_dim / 2) continue;
+    double w = std::pow(base, -2.0 * j / r.rot_dim);   // radians a position
+    if (r.scaling == PBT_ROTARY_SCALE_LINEAR) w /= r.factor;
+    if (r.scaling == PBT_ROTARY_SCALE_RAMP) {
+      const double at = (r.trained_len * w / two_pi - r.low) / (r.high - r.low), keep = at < 0.0 ? 0.0 : at > 1.0 ? 1.0 : at;
+      w *= keep + (1.0 - keep) / r.factor;
+    }
+    f->turns[j] = w / two_pi;
+  }
+}
 
 hipError_t rotary_plan(const RotaryFrequencies& f, int n, double* table, hipStream_t s) {
   hipLaunchKernelGGL(rotary_plan_kernel, dim3(1), dim3(256), 0, s, f, n, table);

@@ -9,6 +9,7 @@
 
 #include "dense_host.h"
 #include "gemm_choose.h"
+#include "operators.h"
 
 namespace pbt {
 
@@ -109,6 +110,74 @@ pbt_status ln_backward(const Ctx& x, LnLate* late, const bf16_t* dy, const bf16_
   return PBT_OK;
 }
 
+// Query and key heads of rows [P * n][3 d] turned by their positions in place; backward: the transposed rotation, on their gradients.
+pbt_status turn_heads(const Ctx& x, bf16_t* qkv, int backward) {
+  const TfPlan& t = x.h->plan.tf;
+  if (!t.opt.rotary) return PBT_OK;
+  const Dim& D = x.D;
+  RotaryArgs a{};
+  a.g[0] = pbt_heads{qkv, qkv, 3 * D.d, D.dh, 3 * D.d, D.dh, 2 * D.H, 0};
+  a.n_groups = 1; a.heads = 2 * D.H;
+  a.rows = (int64_t)x.P * x.n; a.width = D.dh; a.rot = t.opt.rot.rot_dim;
+  a.period = D.S;   // (rows are whole sequences)
+  a.gain = (float)t.opt.rot.gain; a.sign = backward ? -1.f : 1.f;
+  a.turns = x.h->st<double>(t.o_turns);
+  PBT_LAUNCH(x.h, PBT_K_HEAD, x.s, rotary_apply(a, t.opt.rot.layout, PBT_DTYPE_BF16, x.s));
+  return PBT_OK;
+}
+
+// The block norm that closes branch k of block l (0: attention, 1: feed-forward): its input, the stream it is added to, where the stream goes on, and the
+// LayerNorm that follows (the block's second, the next block's first, the last one).
+struct BlockSite { bf16_t *y, *x, *out, *z; float* stats; int64_t post, gate, g, b; };
+BlockSite block_site(const Ctx& x, int l, int k) {
+  const TfPlan& t = x.h->plan.tf;
+  const TfBlockOff& o = t.blk[l];
+  const bool last = l + 1 == x.D.L;
+  BlockSite s;
+  s.y = x.sc<bf16_t>(t.o_y[l][k]);
+  s.stats = x.sc<float>(t.o_bnstats[l][k]);
+  s.post = o.post[k]; s.gate = o.gate[k];
+  s.x = x.sc<bf16_t>(k == 0 ? t.o_h[l] : t.o_hmid[l]);
+  s.out = x.sc<bf16_t>(k == 0 ? t.o_hmid[l] : t.o_h[l + 1]);
+  s.z = x.sc<bf16_t>(k == 0 ? t.o_u2[l] : last ? t.o_uf : t.o_u[l + 1]);
+  s.g = k == 0 ? o.ln2g : last ? t.lnfg : t.blk[l + 1].ln1g;
+  s.b = k == 0 ? o.ln2b : last ? t.lnfb : t.blk[l + 1].ln1b;
+  return s;
+}
+BlockArgs block_args(const Ctx& x, const BlockSite& s) {
+  const pbt_tf_options& o = x.h->plan.tf.opt;
+  BlockArgs a{};
+  a.n = pbt_block_norm{x.n, x.P, x.D.d, o.block_norm, PBT_NORM_LAYER, PBT_GATE_VECTOR, PBT_ACT_NONE, PBT_DTYPE_BF16, PBT_DTYPE_BF16, 1e-5f, o.alpha, o.beta};
+  float* w = const_cast<float*>(x.W32);
+  a.p = pbt_block_params{w + s.post, nullptr, w + s.g, w + s.b, w + s.gate, x.S_};
+  a.y = pbt_rows{s.y, x.D.d}; a.x = pbt_rows{s.x, x.D.d};
+  a.stats = s.stats;
+  return a;
+}
+// tmp: the branch's product; drop: its dropout site is active
+pbt_status block_forward(const Ctx& x, int l, int k, const bf16_t* tmp, const DropArgs& dr, bool drop) {
+  const BlockSite s = block_site(x, l, k);
+  const TfPlan& t = x.h->plan.tf;
+  if (drop) PBT_HIP(x.h, dropout_apply(tmp, nullptr, x.P, (int64_t)x.n * x.D.d, dr, 4 * l + 1 + 2 * k, s.y, x.s, nullptr, x.sc<uint16_t>(t.o_mask[l][2 * k])));
+  BlockArgs a = block_args(x, s);
+  a.out = pbt_rows{s.out, x.D.d}; a.z = pbt_rows{s.z, x.D.d};
+  PBT_HIP(x.h, block_norm_forward(a, x.s));
+  return PBT_OK;
+}
+// dz: gradient of the LayerNorm's rows; dout: of the stream behind the branch (null: none but dz's); dx: of the stream before it, dd: of the branch's product
+pbt_status block_backward(const Ctx& x, int l, int k, bf16_t* dz, bf16_t* dout, bf16_t* dx, bf16_t* dd, const DropArgs& dr, bool drop) {
+  const BlockSite s = block_site(x, l, k);
+  const TfPlan& t = x.h->plan.tf;
+  BlockArgs a = block_args(x, s);
+  a.g = pbt_block_params{x.G + s.post, nullptr, x.G + s.g, x.G + s.b, x.G + s.gate, x.S_};
+  a.dz = pbt_rows{dz, x.D.d}; a.dout = pbt_rows{dout, x.D.d};
+  a.dx = pbt_rows{dx, x.D.d}; a.dy = pbt_rows{drop ? dz : dd, x.D.d};   // (over dz, which nothing reads again)
+  a.part = x.sc<float>(t.o_bnwork);
+  PBT_HIP(x.h, block_norm_backward(a, x.s));
+  if (drop) PBT_HIP(x.h, dropout_apply(dz, nullptr, x.P, (int64_t)x.n * x.D.d, dr, 4 * l + 1 + 2 * k, dd, x.s, x.sc<uint16_t>(t.o_mask[l][2 * k])));
+  return PBT_OK;
+}
+
 // One attention product over all (member, sequence, head) triples.  Operands live inside
 // [P*Bc][S][pitch] arrays at column `col` + head * dh, or inside the [P*Bc][H][S][S] score arrays.
 struct Opnd { const bf16_t* p; int64_t pitch, outer, inner; };
@@ -130,7 +199,7 @@ pbt_status forward(const Ctx& x, const int32_t* pool, int n_pool, uint32_t c0, i
   const Dim& D = x.D;
   const DropArgs dr{h->st<float>(h->plan.o_hyper), c.n_hyper, t.col_drop, train, c0, c.seed};
   const int64_t per_d = (int64_t)x.n * D.d, per_f = (int64_t)x.n * D.f;
-  PBT_LAUNCH(h, PBT_K_FETCH, x.s, embed_fwd(pool, n_pool, D.S, x.Bc, D.d, D.V, x.P, x.W16, x.S_, t.tok, t.pos, c0, c.seed, draw,
+  PBT_LAUNCH(h, PBT_K_FETCH, x.s, embed_fwd(pool, n_pool, D.S, x.Bc, D.d, D.V, x.P, x.W16, x.S_, t.tok, t.opt.learned_positions ? t.pos : -1, c0, c.seed, draw,
                                             x.sc<bf16_t>(t.o_h[0]), x.sc<int32_t>(t.o_tokens), x.sc<int32_t>(t.o_targets),
                                             h->st<int32_t>(h->plan.o_t), x.s));
   bf16_t* tmp_d = x.sc<bf16_t>(t.o_tmp_d[0]);
@@ -149,6 +218,7 @@ pbt_status forward(const Ctx& x, const int32_t* pool, int n_pool, uint32_t c0, i
     if (!x.fused_bwd || l == 0)
       PBT_HIP(h, layernorm_fwd(hin, x.P, x.n, D.d, x.W32, x.S_, b.ln1g, b.ln1b, u, x.sc<float>(t.o_mean1[l]), x.sc<float>(t.o_rstd1[l]), x.s));
     TF_TRY(dense(x, u, D.d, 3 * D.d, b.wqkv, b.bqkv, nullptr, qkv, PBT_ACT_NONE));
+    TF_TRY(turn_heads(x, qkv, 0));
     if (t.fused_attn) {
       PBT_LAUNCH(h, PBT_K_HEAD, x.s, attention_fwd(qkv, x.P, x.Bc, D.S, D.d, D.H, 1.f / sqrtf((float)D.dh), dr, 4 * l + 0, o,
                                                    train ? x.sc<uint32_t>(t.o_keep[l]) : nullptr, x.s));
@@ -157,9 +227,19 @@ pbt_status forward(const Ctx& x, const int32_t* pool, int n_pool, uint32_t c0, i
       PBT_HIP(h, softmax_fwd(score, x.P, (int64_t)x.Bc * D.H * D.S, D.S, 1.f / sqrtf((float)D.dh), dr, 4 * l + 0, pq, pd, x.s));
       TF_TRY(attn_gemm(x, in_scores(pd, D), false, in_rows(qkv, 2 * D.d, 3 * D.d, D), false, in_rows(o, 0, D.d, D), D.S, D.dh, D.S));
     }
-    TF_TRY(dense(x, o, D.d, D.d, b.wo, b.bo, nullptr, tmp_d, PBT_ACT_NONE));
+    const bool normed = t.opt.block_norm != PBT_NORM_NONE, drop = t.col_drop >= 0 && train;
+    TF_TRY(dense(x, o, D.d, D.d, b.wo, b.bo, nullptr, normed && !drop ? x.sc<bf16_t>(t.o_y[l][0]) : tmp_d, PBT_ACT_NONE));
     bf16_t* u2 = x.sc<bf16_t>(t.o_u2[l]);
     bf16_t* fd = x.sc<bf16_t>(t.o_fd[l]);
+    if (normed) {
+      TF_TRY(block_forward(x, l, 0, tmp_d, dr, drop));
+      DropSite site;
+      if (train) site = DropSite{dr, 4 * l + 2, x.sc<uint8_t>(t.o_mask[l][1]), (int64_t)dropout_mask_bytes(1, per_f)};
+      TF_TRY(dense(x, u2, D.d, D.f, b.w1, b.b1, nullptr, fd, PBT_ACT_RELU, site));
+      TF_TRY(dense(x, fd, D.f, D.d, b.w2, b.b2, nullptr, drop ? tmp_d : x.sc<bf16_t>(t.o_y[l][1]), PBT_ACT_NONE));
+      TF_TRY(block_forward(x, l, 1, tmp_d, dr, drop));
+      continue;
+    }
     if (x.fused_bwd) {
       // residual + dropout + the next LayerNorm in one kernel; the feed-forward hidden layer's dropout in the epilogue of
       // its GEMM (only the dropped-out activation is kept: it is positive exactly where the pre-activation is positive and
@@ -205,6 +285,22 @@ Ctx make_ctx(pbt_handle* h, int Bc, hipStream_t s) {
 
 }  // namespace
 
+pbt_status tf_check_options(const pbt_config* c, const pbt_tf_options* o) {
+  if (c->workload != PBT_WL_TRANSFORMER) return fail(nullptr, PBT_EINVAL, "transformer options need the transformer workload");
+  if ((o->rotary != 0 && o->rotary != 1) || (o->learned_positions != 0 && o->learned_positions != 1)) return fail(nullptr, PBT_EINVAL, "rotary / learned_positions are 0 or 1");
+  if (o->block_norm < PBT_NORM_NONE || o->block_norm > PBT_NORM_RMS) return fail(nullptr, PBT_EINVAL, "unknown norm %d", o->block_norm);
+  if (o->unused != 0) return fail(nullptr, PBT_EINVAL, "the unused field must be 0");
+  if (!std::isfinite(o->alpha) || !std::isfinite(o->beta)) return fail(nullptr, PBT_EINVAL, "alpha and beta must be finite");
+  if (o->block_norm == PBT_NORM_NONE && (o->alpha != 1.f || o->beta != 1.f)) return fail(nullptr, PBT_EINVAL, "alpha and beta other than 1 need a block norm");
+  if (o->block_norm != PBT_NORM_NONE && !tf_fused_elementwise(*c)) return fail(nullptr, PBT_EUNSUPPORTED, "block norms are built for d_model up to 2048");
+  if (o->rotary) {
+    const pbt_status st = check_rotary(&o->rot);
+    if (st != PBT_OK) return st;
+    if (c->tf_heads < 1 || o->rot.rot_dim > c->tf_d_model / c->tf_heads) return fail(nullptr, PBT_EINVAL, "rot_dim = %d is more than a head", o->rot.rot_dim);
+  }
+  return PBT_OK;
+}
+
 pbt_status tf_layout(const pbt_config* c, Plan* pl) {
   const int L = c->n_layers;
   if (c->tf_vocab < 2 || c->tf_d_model < 8 || c->tf_heads < 1 || c->tf_d_ff < 8 || c->tf_seq < 1)
@@ -213,7 +309,8 @@ pbt_status tf_layout(const pbt_config* c, Plan* pl) {
     return fail(nullptr, PBT_EUNSUPPORTED, "d_model, head width, d_ff, vocabulary and sequence length must be multiples of 8");
   if (c->tf_seq > 4096) return fail(nullptr, PBT_EUNSUPPORTED, "sequence length above 4096");
   if ((int64_t)c->batch * c->tf_seq > 16000) return fail(nullptr, PBT_EUNSUPPORTED, "more than 16000 positions per member and step");
-  if (2 + 12 * L + 4 > PBT_MAX_SEGMENTS || L >= PBT_MAX_DIMS) return fail(nullptr, PBT_EUNSUPPORTED, "too many blocks");
+  const bool normed = pl->tf.opt.block_norm != PBT_NORM_NONE;
+  if (2 + (normed ? 16 : 12) * L + 4 > PBT_MAX_SEGMENTS || L >= PBT_MAX_DIMS) return fail(nullptr, PBT_EUNSUPPORTED, "too many blocks");
   pbt_layout& lay = pl->lay;
   TfPlan& t = pl->tf;
   std::memset(&lay, 0, sizeof lay);
@@ -233,6 +330,7 @@ pbt_status tf_layout(const pbt_config* c, Plan* pl) {
     TfBlockOff& b = t.blk[l];
     b.ln1g = seg(d); b.ln1b = seg(d); b.wqkv = seg(d * 3 * d); b.bqkv = seg(3 * d); b.wo = seg(d * d); b.bo = seg(d);
     b.ln2g = seg(d); b.ln2b = seg(d); b.w1 = seg(d * f); b.b1 = seg(f); b.w2 = seg(f * d); b.b2 = seg(d);
+    for (int k = 0; k < 2 && normed; ++k) { b.post[k] = seg(d); b.gate[k] = seg(d); }
   }
   t.lnfg = seg(d); t.lnfb = seg(d); t.whead = seg(d * V); t.bhead = seg(V);
   lay.stride = round_up(off, STRIDE_ALIGN);
@@ -265,8 +363,17 @@ pbt_status tf_check_and_plan(const pbt_config* c, Plan* pl, Carver* w) {
     t.o_mask[l][0] = w->take(dropout_mask_bytes((int)P, (int64_t)n * D.d));
     t.o_mask[l][1] = w->take(dropout_mask_bytes((int)P, (int64_t)n * D.f));
     t.o_mask[l][2] = w->take(dropout_mask_bytes((int)P, (int64_t)n * D.d));
+    for (int k = 0; k < 2; ++k) {
+      t.o_y[l][k] = t.opt.block_norm != PBT_NORM_NONE ? w->take(nd) : 0;
+      t.o_bnstats[l][k] = t.opt.block_norm != PBT_NORM_NONE ? w->take(P * n * 16) : 0;
+    }
   }
   t.o_meanf = w->take(P * n * 4); t.o_rstdf = w->take(P * n * 4);
+  t.o_bnwork = 0;
+  if (t.opt.block_norm != PBT_NORM_NONE) {
+    const pbt_block_norm bn{(int64_t)n, c->P, D.d, t.opt.block_norm, PBT_NORM_LAYER, PBT_GATE_VECTOR, PBT_ACT_NONE, PBT_DTYPE_BF16, PBT_DTYPE_BF16, 1e-5f, t.opt.alpha, t.opt.beta};
+    t.o_bnwork = w->take(block_norm_work_bytes(bn));
+  }
   t.o_score = t.fused_attn ? 0 : w->take(ns);
   t.o_attn_stats = t.fused_attn ? w->take(attention_stats_bytes((int)P, c->batch, D.H, D.S)) : 0;
   for (int k = 0; k < 3; ++k) t.o_tmp_d[k] = w->take(nd);
@@ -326,11 +433,15 @@ pbt_status tf_step(pbt_handle* h, const int32_t* pool, uint32_t step, hipStream_
   };
   const bool fb = x.fused_bwd;
   LnLate sums, *late = ln_late(x, &sums) ? &sums : nullptr;
+  const bool normed = t.opt.block_norm != PBT_NORM_NONE, drop = t.col_drop >= 0;
   // head and final LayerNorm
   TF_TRY(wgrad(x, x.sc<bf16_t>(t.o_uf), D.d, dl, D.V, t.whead, t.bhead));
   TF_TRY(dgrad(x, dl, D.V, D.d, t.whead, nullptr, 0, du));   // (du: the final LayerNorm's output buffer, free once the head's weight gradient is taken)
-  TF_TRY(ln_backward(x, late, du, x.sc<bf16_t>(t.o_h[D.L]), x.sc<float>(t.o_meanf), x.sc<float>(t.o_rstdf), t.lnfg, t.lnfb, nullptr, dh,
-                     fb ? dd : nullptr, fb ? record(D.L - 1, 2, per_d) : DropRecord()));
+  if (normed)
+    TF_TRY(block_backward(x, D.L - 1, 1, du, nullptr, dh, dd, dr, drop));
+  else
+    TF_TRY(ln_backward(x, late, du, x.sc<bf16_t>(t.o_h[D.L]), x.sc<float>(t.o_meanf), x.sc<float>(t.o_rstdf), t.lnfg, t.lnfb, nullptr, dh,
+                       fb ? dd : nullptr, fb ? record(D.L - 1, 2, per_d) : DropRecord()));
   for (int l = D.L - 1; l >= 0; --l) {
     const TfBlockOff& b = t.blk[l];
     bf16_t* qkv = x.sc<bf16_t>(t.o_qkv[l]);
@@ -345,8 +456,11 @@ pbt_status tf_step(pbt_handle* h, const int32_t* pool, uint32_t step, hipStream_
     }
     TF_TRY(wgrad(x, x.sc<bf16_t>(t.o_u2[l]), D.d, df1, D.f, b.w1, b.b1));
     TF_TRY(dgrad(x, df1, D.f, D.d, b.w1, nullptr, 0, du));
-    TF_TRY(ln_backward(x, late, du, x.sc<bf16_t>(t.o_hmid[l]), x.sc<float>(t.o_mean2[l]), x.sc<float>(t.o_rstd2[l]), b.ln2g, b.ln2b, dh, dh2,
-                       fb ? dd : nullptr, fb ? record(l, 0, per_d) : DropRecord()));
+    if (normed)
+      TF_TRY(block_backward(x, l, 0, du, dh, dh2, dd, dr, drop));
+    else
+      TF_TRY(ln_backward(x, late, du, x.sc<bf16_t>(t.o_hmid[l]), x.sc<float>(t.o_mean2[l]), x.sc<float>(t.o_rstd2[l]), b.ln2g, b.ln2b, dh, dh2,
+                         fb ? dd : nullptr, fb ? record(l, 0, per_d) : DropRecord()));
     // attention branch
     if (!fb) PBT_HIP(h, dropout_apply(dh2, nullptr, x.P, per_d, dr, 4 * l + 1, dd, s, x.sc<uint16_t>(t.o_mask[l][0])));
     TF_TRY(wgrad(x, x.sc<bf16_t>(t.o_o[l]), D.d, dd, D.d, b.wo, b.bo));
@@ -362,18 +476,24 @@ pbt_status tf_step(pbt_handle* h, const int32_t* pool, uint32_t step, hipStream_
       TF_TRY(attn_gemm(x, in_scores(dscore, D), false, in_rows(qkv, D.d, 3 * D.d, D), false, in_rows(dqkv, 0, 3 * D.d, D), D.S, D.dh, D.S));       // dQ = dS K
       TF_TRY(attn_gemm(x, in_scores(dscore, D), true, in_rows(qkv, 0, 3 * D.d, D), false, in_rows(dqkv, D.d, 3 * D.d, D), D.S, D.dh, D.S));        // dK = dS^T Q
     }
+    TF_TRY(turn_heads(x, dqkv, 1));
     TF_TRY(wgrad(x, x.sc<bf16_t>(t.o_u[l]), D.d, dqkv, 3 * D.d, b.wqkv, b.bqkv));
     TF_TRY(dgrad(x, dqkv, 3 * D.d, D.d, b.wqkv, nullptr, 0, du));
+    if (normed && l > 0) {
+      TF_TRY(block_backward(x, l - 1, 1, du, dh2, dh, dd, dr, drop));
+      continue;
+    }
     const bool next = fb && l > 0;   // the block below starts with the backward of its feed-forward output site
     TF_TRY(ln_backward(x, late, du, x.sc<bf16_t>(t.o_h[l]), x.sc<float>(t.o_mean1[l]), x.sc<float>(t.o_rstd1[l]), b.ln1g, b.ln1b, dh2, dh,
                        next ? dd : nullptr, next ? record(l - 1, 2, per_d) : DropRecord()));
   }
   if (late) PBT_HIP(h, layernorm_param_combine(late->part, late->stride, late->n, late->g, late->b, layernorm_bwd_slabs(x.n), x.P, D.d, x.G, x.S_, s));
-  PBT_HIP(h, embed_bwd(dh, x.sc<int32_t>(t.o_tokens), x.Bc, D.S, D.d, D.V, x.P, x.G, x.S_, t.tok, t.pos, x.sc<int32_t>(t.o_tokends),
+  PBT_HIP(h, embed_bwd(dh, x.sc<int32_t>(t.o_tokens), x.Bc, D.S, D.d, D.V, x.P, x.G, x.S_, t.tok, t.opt.learned_positions ? t.pos : -1, x.sc<int32_t>(t.o_tokends),
                        x.sc<int32_t>(t.o_tokorder), s));
   OptArgs oa{h->st<float>(p.o_w32), h->st<float>(p.o_opt0), h->st<float>(p.o_opt1), h->st<bf16_t>(p.o_w16), x.G, 0, x.S_,
              h->st<float>(p.o_hyper), h->st<int32_t>(p.o_t), x.S_, x.P, c.n_hyper, PBT_OPT_ADAM, p.col_lr, -1, -1,
              c.opt_const[0], c.opt_const[1], c.opt_const[2], c.opt_const[3]};
+  TF_TRY(clip_step(h, &oa, s));
   PBT_LAUNCH(h, PBT_K_OPTIMIZER, s, optimizer_step(oa, s));
   return PBT_OK;
 }

@@ -37,7 +37,7 @@ __device__ __forceinline__ void store8(bf16_t* p, const float* v) {
 }
 
 // ---- embeddings ------------------------------------------------------------------------------
-// h[i][b][s][:] = tok[token] + pos[s]; tokens are drawn here: sequence b of member i is pool row
+// h[i][b][s][:] = tok[token] + pos[s] (pos_off < 0: without positions); tokens are drawn here: sequence b of member i is pool row
 // floor(x * n_pool / 2^32), x from Philox domain 1; also copies the targets and bumps t.
 // A wavefront per position, eight elements (16 bytes) per lane and pass: 65536 rows of 512 in 35 us (47 with 2-byte accesses).
 __global__ __launch_bounds__(256) void embed_fwd_kernel(const int32_t* __restrict__ pool, int n_pool, int S, int B, int d, int V,
@@ -58,9 +58,11 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const int32_t* __restric
   for (int c = lane * 8; c < d; c += 512) {
     float v[8], w[8];
     load8(te + c, v);
-    load8(pe + c, w);
+    if (pos_off >= 0) {
+      load8(pe + c, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w[e];
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
+    }
     store8(h + r * d + c, v);
   }
   if (lane == 0) {
@@ -72,7 +74,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const int32_t* __restric
 hipError_t embed_fwd(const int32_t* pool, int n_pool, int S, int B, int d, int V, int P, const bf16_t* W16, int64_t stride,
                      int64_t tok_off, int64_t pos_off, uint32_t c0, uint64_t seed, int draw, bf16_t* h, int32_t* tokens,
                      int32_t* targets, int32_t* t, hipStream_t s) {
-  if (d % 8 || stride % 8 || tok_off % 8 || pos_off % 8) return hipErrorInvalidValue;
+  if (d % 8 || stride % 8 || tok_off % 8 || (pos_off >= 0 && pos_off % 8)) return hipErrorInvalidValue;
   hipLaunchKernelGGL(embed_fwd_kernel, dim3((unsigned)((B * S + 3) / 4), P), dim3(256), 0, s, pool, n_pool, S, B, d, V, W16, stride, tok_off, pos_off, c0,
                      (uint32_t)seed, (uint32_t)(seed >> 32), draw, h, tokens, targets, t);
   return hipGetLastError();
@@ -222,7 +224,7 @@ hipError_t embed_bwd(const bf16_t* dh, const int32_t* tokens, int B, int S, int 
   const int per = (V + TOK_THREADS - 1) / TOK_THREADS, span = (per < TOK_SPAN ? per : TOK_SPAN) | 1;
   hipLaunchKernelGGL(tok_lists_kernel, dim3(P), dim3(TOK_THREADS), (size_t)TOK_THREADS * span * sizeof(int32_t), s, tokens, n, V, span, ends, order);
   hipLaunchKernelGGL(tok_sum_kernel, dim3(V, P), dim3(128), 0, s, dh, ends, order, n, d, V, G, stride, tok_off);
-  hipLaunchKernelGGL(pos_sum_kernel, dim3(S, P), dim3(128), 0, s, dh, B, S, d, G, stride, pos_off);
+  if (pos_off >= 0) hipLaunchKernelGGL(pos_sum_kernel, dim3(S, P), dim3(128), 0, s, dh, B, S, d, G, stride, pos_off);
   return hipGetLastError();
 }
 

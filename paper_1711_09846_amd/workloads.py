@@ -18,7 +18,7 @@ import numpy as np
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_LEAKY_RELU, ACT_TANH = 0, 1, 2, 3, 4
 OPT_SGD_MOMENTUM, OPT_ADAM, OPT_RMSPROP = 0, 1, 2
 DTYPE_FP32, DTYPE_BF16 = 0, 1
-ROLE_LR, ROLE_BETA1, ROLE_WD, ROLE_LR_G, ROLE_LR_D, ROLE_ENTROPY_COST, ROLE_DROPOUT, ROLE_LABEL_SMOOTH = 0, 1, 2, 3, 4, 5, 6, 7
+ROLE_LR, ROLE_BETA1, ROLE_WD, ROLE_LR_G, ROLE_LR_D, ROLE_ENTROPY_COST, ROLE_DROPOUT, ROLE_LABEL_SMOOTH, ROLE_CLIP_NORM = range(9)
 WL_CLASSIFIER, WL_GAN, WL_TRANSFORMER, WL_A2C = 1, 3, 4, 5
 
 POPULATION_SEED = 2017          # Philox key of the population
@@ -99,21 +99,28 @@ TRANSFORMER = Workload(
 WORKLOADS = {1: MLP_SMALL, 2: MLP_WIDE, 3: GAN_MLP, 4: TRANSFORMER, 5: A2C_MLP}
 
 
+def _block_normed(wl):
+    return (getattr(wl, "tf_options", None) or {}).get("block_norm", "none") != "none"
+
+
 def transformer_shapes(wl):
-    """Shapes of the parameter arrays of one transformer, in the order of the flat parameter vector."""
+    """Shapes of the parameter arrays of one transformer, in the order of the flat parameter vector (tf_options with a block norm: gain and gate
+    of both branches behind every block's arrays)."""
     d, f, V, S = wl.d_model, wl.d_ff, wl.vocab, wl.seq
     out = [(V, d), (S, d)]
+    block = [(d,), (d,), (d, 3 * d), (3 * d,), (d, d), (d,), (d,), (d,), (d, f), (f,), (f, d), (d,)] + [(d,)] * (4 if _block_normed(wl) else 0)
     for _ in range(wl.n_blocks):
-        out += [(d,), (d,), (d, 3 * d), (3 * d,), (d, d), (d,), (d,), (d,), (d, f), (f,), (f, d), (d,)]
+        out += block
     return out + [(d,), (d,), (d, V), (V,)]
 
 
 def initial_transformer_weights(wl, P, seed):
     """Per member the parameter arrays in layout order: embeddings ~ N(0, 0.1^2), matrices uniform in
-    +-1/sqrt(fan_in), LayerNorm gains 1, every bias 0."""
+    +-1/sqrt(fan_in), gains and gates 1, every bias 0."""
     rng = np.random.default_rng(seed)
     shapes = transformer_shapes(wl)
-    gains = {2 + 12 * l + k for l in range(wl.n_blocks) for k in (0, 6)} | {len(shapes) - 4}
+    per = 16 if _block_normed(wl) else 12
+    gains = {2 + per * l + k for l in range(wl.n_blocks) for k in (0, 6) + tuple(range(12, per))} | {len(shapes) - 4}
     members = []
     for _ in range(P):
         arrays = []
