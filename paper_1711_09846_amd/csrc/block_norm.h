@@ -1,7 +1,7 @@
 // What both passes of the block norms share (block_norm_forward.hip, block_norm_backward.hip): how a row lies over threads, sums over a row, the gate.
 //
-// A thread has eight consecutive elements of a row in registers, so that a row is read once whatever is summed over it.  A team of T threads has a row: T = 16
-// (rows of up to 128 elements, four a wavefront), a wavefront (up to 512), or as many wavefronts as the row needs, one workgroup (WIDE, up to 16
+// A thread has eight consecutive elements of a row in registers, so that a row is read once whatever is summed over it.  A team of T threads has a row: 8, 16 or 32 of a
+// wavefront's (rows of up to 64, 128, 256 elements), a wavefront (up to 512), or as many wavefronts as the row needs, one workgroup (WIDE, up to 16
 // wavefronts).  A workgroup takes a slab of a member's rows; a thread keeps the same columns for all of them, so parameters are read once a slab and
 // their gradients add up in registers.  The next row is requested as soon as this one's values have been taken over: loads are single instructions without a
 // branch around their results, which the compiler would wait at (with such branches 8191 rows of 5001 took 129 us forward, 94 now).
@@ -15,30 +15,38 @@ namespace pbt {
 constexpr int WIDE = 0;   // T of a team that is the whole workgroup
 struct BlockTeam { int T, threads, rows; };   // threads of a workgroup, rows it has at a time
 inline BlockTeam block_team(int d) {
+  if (d <= 64) return {8, 256, 32};
   if (d <= 128) return {16, 256, 16};
+  if (d <= 256) return {32, 256, 8};
   if (d <= 512) return {64, 256, 4};
   return {WIDE, (d + 511) / 512 * 64, 1};
 }
 
 // Rows of a slab.  What a slab costs besides its rows (`extra` bytes a column: parameters read, sums written and read again) should be an eighth of what
 // its rows move (`moved` bytes a column and row) and a team should see eight rows, while every compute unit has `resident` workgroups, and there
-// are at most 16 for every compute unit.
-inline int64_t slab_rows(const pbt_block_norm& n, int extra, int moved, int resident) {
+// are at most `most` in all.
+inline int64_t slab_rows(const pbt_block_norm& n, int extra, int moved, int resident, int most) {
   const BlockTeam t = block_team(n.d);
   const int64_t all = n.rows * n.P;
   int64_t rows = std::max<int64_t>((8 * extra + moved - 1) / moved, 8 * t.rows);
   rows = std::min(rows, (all + 256 * resident - 1) / (256 * resident));   // (rounded up: a few workgroups more than fit would double the time)
-  rows = std::max(rows, (all + 4095) / 4096);
+  rows = std::max(rows, (all + most - 1) / most);
   rows = (rows + t.rows - 1) / t.rows * t.rows;
   return std::max<int64_t>(std::min(rows, n.rows), 1);
 }
 
-__device__ __forceinline__ float2 sum16(float2 v) {   // over rows of 16 lanes
+// over T = 8, 16 or 32 adjacent lanes: quads change places, half rows are mirrored (quads are equal by then), rows of 16 are mirrored, two rows are swapped
+template <int T>
+__device__ __forceinline__ float lanes_sum(float v) {
   const auto f = [](float x, auto ctrl) { return x + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
-  v.x = f(v.x, std::integral_constant<int, 0x128>()); v.y = f(v.y, std::integral_constant<int, 0x128>());
-  v.x = f(v.x, std::integral_constant<int, 0x124>()); v.y = f(v.y, std::integral_constant<int, 0x124>());
-  v.x = f(v.x, std::integral_constant<int, 0x4e>()); v.y = f(v.y, std::integral_constant<int, 0x4e>());
-  v.x = f(v.x, std::integral_constant<int, 0xb1>()); v.y = f(v.y, std::integral_constant<int, 0xb1>());
+  v = f(v, std::integral_constant<int, 0xb1>());             // quad_perm [1, 0, 3, 2]
+  v = f(v, std::integral_constant<int, 0x4e>());             // quad_perm [2, 3, 0, 1]
+  v = f(v, std::integral_constant<int, 0x141>());            // row_half_mirror
+  if (T >= 16) v = f(v, std::integral_constant<int, 0x140>());   // row_mirror
+  if (T >= 32) {
+    const auto g = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(g[0]) + __uint_as_float(g[1]);
+  }
   return v;
 }
 
@@ -47,8 +55,7 @@ __device__ __forceinline__ float2 sum16(float2 v) {   // over rows of 16 lanes
 template <int T> struct TeamSum {
   __device__ __forceinline__ TeamSum(float2*) {}
   __device__ __forceinline__ float2 operator()(float a, float b) {
-    if (T == 16) return sum16(make_float2(a, b));
-    return make_float2(wave_sum(a), wave_sum(b));
+    return T < 64 ? make_float2(lanes_sum<T>(a), lanes_sum<T>(b)) : make_float2(wave_sum(a), wave_sum(b));
   }
 };
 template <> struct TeamSum<WIDE> {
@@ -65,7 +72,8 @@ template <> struct TeamSum<WIDE> {
     half ^= 1;
     if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = make_float2(a, b);
     __syncthreads();
-    return sum16(r[threadIdx.x & 15]);
+    const float2 v = r[threadIdx.x & 15];
+    return make_float2(lanes_sum<16>(v.x), lanes_sum<16>(v.y));
   }
 };
 

@@ -193,15 +193,12 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
   float* part = a.part + ((int64_t)i * gridDim.x + blockIdx.x) * SUMS * k.d;
   if (T != WIDE) {
     // the teams of a workgroup add theirs up: those of a wavefront across its lanes, then the wavefronts in turn
-    if (T == 16) {
+#pragma unroll
+    for (int by = T; by < 64; by *= 2)
 #pragma unroll
       for (int q = 0; q < SUMS; ++q)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          acc[q][e] += __shfl_xor(acc[q][e], 16);
-          acc[q][e] += __shfl_xor(acc[q][e], 32);
-        }
-    }
+        for (int e = 0; e < 8; ++e) acc[q][e] += __shfl_xor(acc[q][e], by);
     const int wave = threadIdx.x >> 6;
     __syncthreads();   // (the parameters in LDS have been used)
     for (int turn = 0; turn < 4; ++turn) {
@@ -256,7 +253,7 @@ int64_t rows_per_slab(const pbt_block_norm& n) {
   const int a = n.dtype == PBT_DTYPE_BF16 ? 2 : 4, r = n.res_dtype == PBT_DTYPE_BF16 ? 2 : 4;
   const int norms = (n.post != PBT_NORM_NONE) + (n.pre != PBT_NORM_NONE), sums = 2 * norms + (n.gate == PBT_GATE_VECTOR);
   const int moved = (n.pre != PBT_NORM_NONE ? 3 : 2) * a + (n.gate == PBT_GATE_ROWS ? 2 * a : 0) + 3 * r;
-  return slab_rows(n, 4 * sums + 8 * sums, moved, std::max(8 / (block_team(n.d).threads / 64), 1));
+  return slab_rows(n, 4 * sums + 8 * sums, moved, std::max(8 / (block_team(n.d).threads / 64), 1), 2048);
 }
 int64_t slabs_of(const pbt_block_norm& n) { return (n.rows + rows_per_slab(n) - 1) / rows_per_slab(n); }
 
@@ -276,7 +273,9 @@ hipError_t launch(const BlockArgs& a, int64_t slabs, hipStream_t s) {
   const int64_t per_slab = rows_per_slab(a.n);
   const dim3 grid((unsigned)slabs, a.n.P), block(t.threads);
   const size_t lds = (size_t)(t.T == WIDE ? PARAMS : SUMS) * 2 * (t.T == WIDE ? t.threads : t.T) * sizeof(float4);
-  if (a.n.d < 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, true, true>), grid, block, lds, s, a, per_slab);
+  if (a.n.d < 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, true, true>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, false, true>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 32) hipLaunchKernelGGL((block_backward_kernel<A, R, 32, 256, false, true>), grid, block, lds, s, a, per_slab);
   else if (t.T == 16) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, false, true>), grid, block, lds, s, a, per_slab);
   else if (t.T == 64) hipLaunchKernelGGL((block_backward_kernel<A, R, 64, 256, false, true>), grid, block, lds, s, a, per_slab);
   else if (t.threads <= 512) return launch_wide<A, R, 512, true>(a, per_slab, grid, block, lds, s);

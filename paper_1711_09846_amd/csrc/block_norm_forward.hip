@@ -84,9 +84,11 @@ void launch(const BlockArgs& a, hipStream_t s) {
   int extra = 0;
   for (const float* p : {a.p.post_gain, a.p.post_bias, a.p.pre_gain, a.p.pre_bias, a.p.gate}) extra += p ? 4 : 0;
   const int moved = (int)((a.n.pre != PBT_NORM_NONE ? 2 : 1) * sizeof(A) + (a.n.gate == PBT_GATE_ROWS ? sizeof(A) : 0) + 2 * sizeof(R));
-  const int64_t per_slab = slab_rows(a.n, extra, moved, std::max(16 / (t.threads / 64), 1));
+  const int64_t per_slab = slab_rows(a.n, extra, moved, std::max(16 / (t.threads / 64), 1), 4096);
   const dim3 grid((unsigned)((a.n.rows + per_slab - 1) / per_slab), a.n.P), block(t.threads);
-  if (a.n.d < 8) hipLaunchKernelGGL((block_forward_kernel<A, R, 16, 256, true>), grid, block, 0, s, a, per_slab);
+  if (a.n.d < 8) hipLaunchKernelGGL((block_forward_kernel<A, R, 8, 256, true>), grid, block, 0, s, a, per_slab);
+  else if (t.T == 8) hipLaunchKernelGGL((block_forward_kernel<A, R, 8, 256, false>), grid, block, 0, s, a, per_slab);
+  else if (t.T == 32) hipLaunchKernelGGL((block_forward_kernel<A, R, 32, 256, false>), grid, block, 0, s, a, per_slab);
   else if (t.T == 16) hipLaunchKernelGGL((block_forward_kernel<A, R, 16, 256, false>), grid, block, 0, s, a, per_slab);
   else if (t.T == 64) hipLaunchKernelGGL((block_forward_kernel<A, R, 64, 256, false>), grid, block, 0, s, a, per_slab);
   else if (t.threads <= 512) hipLaunchKernelGGL((block_forward_kernel<A, R, WIDE, 512, false>), grid, block, 0, s, a, per_slab);
