@@ -377,11 +377,12 @@ pbt_status pbt_batched_gemm_bf16(const void* d_a, int64_t lda, int64_t stride_a,
 /* The gradient norm of every member over all its tensors, and clipping (Pascanu et al. 2013):
  *   norm_i = sqrt(sum over tensors and elements of g^2),   g <- g max_i / norm_i  where norm_i > max_i.
  * h_grads[k]: [P][len] elements, members src_stride (dst_stride) apart; dst may be src (with the same stride: clipped in
- * place), otherwise the two do not overlap and members below their bound are copied.  The largest norm of member i is read on the
+ * place), otherwise the two do not overlap and members below their bound are copied; no dst shares
+ * elements with another tensor.  The largest norm of member i is read on the
  * device, d_max_norm[i * max_norm_stride] (so a column of PBT_ARR_HYPER serves; a stride of 0: one bound for all);
  * NULL: norms only, dst is not looked at.  d_norm (float[P], may be NULL) receives the norm before clipping.
  * Squares are summed in double, in a fixed order: no finite gradient overflows or vanishes.  A member with a NaN has norm NaN and is not
- * scaled; one with an infinity and no NaN has norm infinity and is multiplied by 0; a bound that is NaN does not clip, one below 0 counts as 0.
+ * scaled; the factor is rounded to float; one with an infinity and no NaN has norm infinity and is multiplied by 0; a bound that is NaN does not clip, one below 0 counts as 0.
  * n_grads >= 1, 1 <= P <= PBT_MAX_P, len >= 0.  d_work: at least what pbt_clip_work_bytes says, 8-byte aligned. */
 typedef struct {
   const void* d_src;
@@ -407,7 +408,7 @@ pbt_status pbt_clip_gradients(const pbt_grad* h_grads, int32_t n_grads, int32_t 
 /* Writes the table of frequencies, rot_dim / 2 doubles (in turns per position), that pbt_rotary_apply reads; d_table is 8-byte aligned. */
 pbt_status pbt_rotary_plan(const pbt_rotary* r, void* d_table, size_t table_bytes, void* hip_stream);
 /* One group of heads: element (row, head, e) at d_src[row * src_row + head * src_head + e].  dst is src with the same strides (in
- * place), or the two share no element. */
+ * place), or the two share no element; nor do a dst and another group (at most 32768 heads in all, of at most 16384 elements). */
 typedef struct {
   const void* d_src;
   void* d_dst;
@@ -445,7 +446,7 @@ typedef struct {                    /* device pointers, [P][d] with `stride` ele
   float *post_gain, *post_bias, *pre_gain, *pre_bias, *gate;
   int64_t stride;
 } pbt_block_params;
-/* out may lie over x, z over y (the same pitch).  z (and its fields) is ignored with pre = NONE, gate with gate != ROWS.  d_stats: float[P * rows][4] = {mean, 1 / spread} of y and of
+/* out may lie over x, z over y (the same pitch); statistics, parameters and working memory lie apart from all matrices.  z (and its fields) is ignored with pre = NONE, gate with gate != ROWS.  d_stats: float[P * rows][4] = {mean, 1 / spread} of y and of
  * out, for the backward pass; NULL: not kept. */
 pbt_status pbt_block_norm_forward(const pbt_block_norm* n, const pbt_rows* y, const pbt_rows* x, const pbt_rows* gate, const pbt_block_params* params,
                                   const pbt_rows* out, const pbt_rows* z, float* d_stats, void* hip_stream);

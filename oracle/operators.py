@@ -19,8 +19,9 @@ def clip(grads, max_norm):
     if max_norm is None:
         return norms, None
     m = np.broadcast_to(np.asarray(max_norm, dtype=np.float64), (P,))
+    m = np.where(m < 0.0, 0.0, m)
     with np.errstate(divide="ignore", invalid="ignore"):
-        c = np.where(norms > m, np.maximum(m, 0.0) / norms, 1.0)
+        c = np.where(norms > m, m / norms, 1.0)
         return norms, [np.asarray(g, dtype=np.float64) * c.reshape((P,) + (1,) * (g.ndim - 1)) for g in grads]
 
 

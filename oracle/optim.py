@@ -22,7 +22,8 @@ import numpy as np
 def clip(grads, max_norm):
     """The member's gradient arrays, scaled down to max_norm where their common norm is larger."""
     norm = np.sqrt(sum((g * g).sum() for g in grads))
-    return [g * (max(float(max_norm), 0.0) / norm) for g in grads] if norm > float(max_norm) else grads
+    bound = 0.0 if max_norm < 0 else float(max_norm)
+    return [g * (bound / norm) for g in grads] if norm > bound else grads
 
 
 def sgd_momentum(theta, g, v, lr, mu):

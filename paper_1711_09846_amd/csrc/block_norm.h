@@ -108,32 +108,38 @@ __device__ __forceinline__ void clear_past(float* v, int n) {
   }
 }
 
-// a row's eight elements; TINY: rows of fewer than eight elements
-template <bool TINY, class T>
-__device__ __forceinline__ void load_row(Raw8<T>& r, const T* p, int n) {
-  if (TINY) r.load(p, n);
-  else r.load_end(p, n);
-}
-template <bool TINY, class T>
-__device__ __forceinline__ void get_row(const Raw8<T>& r, float* v, int n) {
-  if (TINY) r.get(v);
-  else get_end(r, v, n);
-}
+// How a wavefront reads a row's eight elements a lane.  The lane at the row's end reads the eight that end there, its neighbours' among them: those must be
+// of the same wavefront, whose loads come before its stores (another one may have written its part already where an output lies over the input).
+// ALONE: widths whose last wavefront has fewer than eight elements in all, which are read one by one.
+inline bool ends_alone(int d) { return d < 8 || (d > 512 && d % 512 > 0 && d % 512 < 8); }
+template <bool ALONE> struct RowReader {
+  bool alone;   // this is that wavefront
+  int n;
+  __device__ __forceinline__ RowReader(int left) : alone(ALONE && __builtin_amdgcn_readfirstlane(left) < 8), n(left) {}
+  template <class T> __device__ __forceinline__ void load(Raw8<T>& r, const T* p) const {
+    if (ALONE && alone) r.load(p, n);
+    else r.load_end(p, n);
+  }
+  template <class T> __device__ __forceinline__ void get(const Raw8<T>& r, float* v) const {
+    if (ALONE && alone) r.get(v);
+    else get_end(r, v, n);
+  }
+};
 
 // Eight parameters of a member from column c, or `otherwise` where there are none; zero past the row's end.  All of a kernel's are requested before the first
 // is looked at.
-template <bool TINY>
-__device__ __forceinline__ void load_param(Raw8<float>& r, const float* p, int64_t stride, int member, int c, int n) {
-  if (p) load_row<TINY>(r, p + member * stride + c, n);
+template <class Reader>
+__device__ __forceinline__ void load_param(const Reader& reader, Raw8<float>& r, const float* p, int64_t stride, int member, int c) {
+  if (p) reader.load(r, p + member * stride + c);
 }
-template <bool TINY>
-__device__ __forceinline__ void get_param(const Raw8<float>& r, const float* p, int n, float otherwise, float* v) {
+template <class Reader>
+__device__ __forceinline__ void get_param(const Reader& reader, const Raw8<float>& r, const float* p, float otherwise, float* v) {
   if (p) {
-    get_row<TINY>(r, v, n);
+    reader.get(r, v);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = otherwise;
-    clear_past(v, n);
+    clear_past(v, reader.n);
   }
 }
 

@@ -26,7 +26,7 @@ __device__ __forceinline__ void to_lds(float4* lds, int stride, int which, int l
 }
 
 // ALL: every parameter's gradient; else those of the two gains only
-template <class A, class R, int T, int MOST, bool TINY, bool ALL>
+template <class A, class R, int T, int MOST, bool ALL, bool ALONE>
 __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64_t rows_per_slab) {
   extern __shared__ float4 lds[];   // [PARAMS][2][threads of a team], then the team's sums
   constexpr int ROWS = T == WIDE ? 1 : 256 / T;
@@ -37,6 +37,7 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
   const pbt_block_norm& k = a.n;
   const float inv_d = 1.f / (float)k.d;
   const int c = l * 8, n = k.d - c;
+  const RowReader<ALONE> reader(n);
   const bool rows_gate = k.gate == PBT_GATE_ROWS, has_dz = a.dz.d != nullptr, has_dout = a.dout.d != nullptr;
   const int64_t r_end = min(k.rows, (int64_t)(blockIdx.x + 1) * rows_per_slab);
   Raw8<A> y, gate, dzr;
@@ -45,13 +46,13 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
   auto fetch = [&](int64_t r) {
     const int64_t row = i * k.rows + r;
     st_next = reinterpret_cast<const float4*>(a.stats)[row];
-    load_row<TINY>(y, row_at<A>(a.y, row) + c, n);
-    load_row<TINY>(x, row_at<R>(a.x, row) + c, n);
-    if (rows_gate) load_row<TINY>(gate, row_at<A>(a.gate, row) + c, n);
-    if (has_dz) load_row<TINY>(dzr, row_at<A>(a.dz, row) + c, n);
+    reader.load(y, row_at<A>(a.y, row) + c);
+    reader.load(x, row_at<R>(a.x, row) + c);
+    if (rows_gate) reader.load(gate, row_at<A>(a.gate, row) + c);
+    if (has_dz) reader.load(dzr, row_at<A>(a.dz, row) + c);
   };
   auto fetch_dout = [&](int64_t r) {
-    if (has_dout) load_row<TINY>(dout, row_at<R>(a.dout, i * k.rows + r) + c, n);
+    if (has_dout) reader.load(dout, row_at<R>(a.dout, i * k.rows + r) + c);
   };
   int64_t r = blockIdx.x * rows_per_slab + group;
   if (r < r_end) {
@@ -63,15 +64,15 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
     const float* const at[4] = {a.p.post_gain, a.p.post_bias, a.p.pre_gain, k.gate == PBT_GATE_VECTOR ? a.p.gate : nullptr};
     float p[8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) load_param<TINY>(raw[q], at[q], a.p.stride, i, c, n);
+    for (int q = 0; q < 4; ++q) load_param(reader, raw[q], at[q], a.p.stride, i, c);
 #pragma unroll
     for (int q = 0; q < 3; ++q) {
-      get_param<TINY>(raw[q], at[q], n, q == 1 ? 0.f : 1.f, p);
+      get_param(reader, raw[q], at[q], q == 1 ? 0.f : 1.f, p);
       to_lds(lds, team, q, l, p);
     }
     if (k.gate == PBT_GATE_VECTOR) {
       float g[8];
-      get_param<TINY>(raw[3], at[3], n, 0.f, g);
+      get_param(reader, raw[3], at[3], 0.f, g);
       gate8<false>(k.gate_act, g, p, nullptr);
     } else {
 #pragma unroll
@@ -89,10 +90,10 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
     const int64_t row = i * k.rows + r;
     const float4 st = st_next;
     float yh[8], xh[8], t[8], f[8], df[8], p[8], q[8];
-    get_row<TINY>(y, yh, n);
-    get_row<TINY>(x, xh, n);
+    reader.get(y, yh);
+    reader.get(x, xh);
     if (rows_gate) {
-      get_row<TINY>(gate, p, n);
+      reader.get(gate, p);
       gate8<true>(k.gate_act, p, f, df);
     } else {
       from_lds(lds, team, 3, l, f);
@@ -121,7 +122,7 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
     float s1 = 0.f, s2 = 0.f;
     if (has_dz) {
       float dz[8];
-      get_row<TINY>(dzr, dz, n);
+      reader.get(dzr, dz);
       from_lds(lds, team, 2, l, p);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
     }
     if (has_dout) {
       float dv[8];
-      get_row<TINY>(dout, dv, n);
+      reader.get(dout, dv);
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[e] += dv[e];
     }
@@ -183,8 +184,8 @@ __global__ __launch_bounds__(MOST) void block_backward_kernel(BlockArgs a, int64
   if (k.gate == PBT_GATE_VECTOR) {
     float g[8], f[8], df[8];
     Raw8<float> raw;
-    load_param<TINY>(raw, a.p.gate, a.p.stride, i, c, n);
-    get_param<TINY>(raw, a.p.gate, n, 0.f, g);
+    load_param(reader, raw, a.p.gate, a.p.stride, i, c);
+    get_param(reader, raw, a.p.gate, 0.f, g);
     gate8<true>(k.gate_act, g, f, df);
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[4][e] *= df[e];
@@ -258,13 +259,13 @@ int64_t rows_per_slab(const pbt_block_norm& n) {
 int64_t slabs_of(const pbt_block_norm& n) { return (n.rows + rows_per_slab(n) - 1) / rows_per_slab(n); }
 
 // more than 64 KB of LDS need a permission, once on every device (wide teams have 72 to 128 KB, whose compute unit has no room for a second of them anyway)
-template <class A, class R, int MOST, bool ALL>
+template <class A, class R, int MOST, bool ALL, bool ALONE>
 hipError_t launch_wide(const BlockArgs& a, int64_t per_slab, dim3 grid, dim3 block, size_t lds, hipStream_t s) {
   if (lds > 64 * 1024) {
-    const hipError_t e = allow_lds<&block_backward_kernel<A, R, WIDE, MOST, false, ALL>>(128 * 1024);
+    const hipError_t e = allow_lds<&block_backward_kernel<A, R, WIDE, MOST, ALL, ALONE>>(128 * 1024);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((block_backward_kernel<A, R, WIDE, MOST, false, ALL>), grid, block, lds, s, a, per_slab);
+  hipLaunchKernelGGL((block_backward_kernel<A, R, WIDE, MOST, ALL, ALONE>), grid, block, lds, s, a, per_slab);
   return hipGetLastError();
 }
 template <class A, class R>
@@ -273,17 +274,19 @@ hipError_t launch(const BlockArgs& a, int64_t slabs, hipStream_t s) {
   const int64_t per_slab = rows_per_slab(a.n);
   const dim3 grid((unsigned)slabs, a.n.P), block(t.threads);
   const size_t lds = (size_t)(t.T == WIDE ? PARAMS : SUMS) * 2 * (t.T == WIDE ? t.threads : t.T) * sizeof(float4);
-  if (a.n.d < 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, true, true>), grid, block, lds, s, a, per_slab);
-  else if (t.T == 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, false, true>), grid, block, lds, s, a, per_slab);
-  else if (t.T == 32) hipLaunchKernelGGL((block_backward_kernel<A, R, 32, 256, false, true>), grid, block, lds, s, a, per_slab);
-  else if (t.T == 16) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, false, true>), grid, block, lds, s, a, per_slab);
-  else if (t.T == 64) hipLaunchKernelGGL((block_backward_kernel<A, R, 64, 256, false, true>), grid, block, lds, s, a, per_slab);
-  else if (t.threads <= 512) return launch_wide<A, R, 512, true>(a, per_slab, grid, block, lds, s);
-  else if (t.threads <= 768) return launch_wide<A, R, 768, true>(a, per_slab, grid, block, lds, s);
+  if (ends_alone(a.n.d)) {
+    if (t.T == WIDE) return launch_wide<A, R, 1024, true, true>(a, per_slab, grid, block, lds, s);
+    hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, true, true>), grid, block, lds, s, a, per_slab);
+  } else if (t.T == 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, true, false>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 32) hipLaunchKernelGGL((block_backward_kernel<A, R, 32, 256, true, false>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 16) hipLaunchKernelGGL((block_backward_kernel<A, R, 16, 256, true, false>), grid, block, lds, s, a, per_slab);
+  else if (t.T == 64) hipLaunchKernelGGL((block_backward_kernel<A, R, 64, 256, true, false>), grid, block, lds, s, a, per_slab);
+  else if (t.threads <= 512) return launch_wide<A, R, 512, true, false>(a, per_slab, grid, block, lds, s);
+  else if (t.threads <= 768) return launch_wide<A, R, 768, true, false>(a, per_slab, grid, block, lds, s);
   // (1024 threads have 128 registers each: with all five sums some go to memory.  2 x 2048 rows of 7000: 155 us with two sums, 282 with five; up to 768
   // threads the number makes no difference)
-  else if (a.g.post_bias || a.g.pre_bias || a.g.gate) return launch_wide<A, R, 1024, true>(a, per_slab, grid, block, lds, s);
-  else return launch_wide<A, R, 1024, false>(a, per_slab, grid, block, lds, s);
+  else if (a.g.post_bias || a.g.pre_bias || a.g.gate) return launch_wide<A, R, 1024, true, false>(a, per_slab, grid, block, lds, s);
+  else return launch_wide<A, R, 1024, false, false>(a, per_slab, grid, block, lds, s);
   return hipGetLastError();
 }
 

@@ -7,7 +7,7 @@
 namespace pbt {
 namespace {
 
-template <class A, class R, int T, int MOST, bool TINY>
+template <class A, class R, int T, int MOST, bool ALONE>
 __global__ __launch_bounds__(MOST) void block_forward_kernel(BlockArgs a, int64_t rows_per_slab) {
   __shared__ float2 red[32];
   TeamSum<T> sum(red);
@@ -16,15 +16,16 @@ __global__ __launch_bounds__(MOST) void block_forward_kernel(BlockArgs a, int64_
   const pbt_block_norm& k = a.n;
   const float d = (float)k.d;
   const int c = l * 8, n = k.d - c;   // the thread's columns, how many of them there are (n <= 0: none)
+  const RowReader<ALONE> reader(n);
   const bool rows_gate = k.gate == PBT_GATE_ROWS;
   const int64_t r_end = min(k.rows, (int64_t)(blockIdx.x + 1) * rows_per_slab);
   Raw8<A> y, gate;
   Raw8<R> x;
   auto fetch = [&](int64_t r) {
     const int64_t row = i * k.rows + r;
-    load_row<TINY>(y, row_at<A>(a.y, row) + c, n);
-    load_row<TINY>(x, row_at<R>(a.x, row) + c, n);
-    if (rows_gate) load_row<TINY>(gate, row_at<A>(a.gate, row) + c, n);
+    reader.load(y, row_at<A>(a.y, row) + c);
+    reader.load(x, row_at<R>(a.x, row) + c);
+    if (rows_gate) reader.load(gate, row_at<A>(a.gate, row) + c);
   };
   int64_t r = blockIdx.x * rows_per_slab + group;
   if (r < r_end) fetch(r);   // (on its way while the parameters are read)
@@ -33,14 +34,14 @@ __global__ __launch_bounds__(MOST) void block_forward_kernel(BlockArgs a, int64_
     Raw8<float> p[5];
     const float* const at[5] = {a.p.post_gain, a.p.post_bias, a.p.pre_gain, a.p.pre_bias, k.gate == PBT_GATE_VECTOR ? a.p.gate : nullptr};
 #pragma unroll
-    for (int q = 0; q < 5; ++q) load_param<TINY>(p[q], at[q], a.p.stride, i, c, n);
-    get_param<TINY>(p[0], at[0], n, 1.f, g1);
-    get_param<TINY>(p[1], at[1], n, 0.f, b1);
-    get_param<TINY>(p[2], at[2], n, 1.f, g2);
-    get_param<TINY>(p[3], at[3], n, 0.f, b2);
+    for (int q = 0; q < 5; ++q) load_param(reader, p[q], at[q], a.p.stride, i, c);
+    get_param(reader, p[0], at[0], 1.f, g1);
+    get_param(reader, p[1], at[1], 0.f, b1);
+    get_param(reader, p[2], at[2], 1.f, g2);
+    get_param(reader, p[3], at[3], 0.f, b2);
     if (k.gate == PBT_GATE_VECTOR) {
       float g[8];
-      get_param<TINY>(p[4], at[4], n, 0.f, g);
+      get_param(reader, p[4], at[4], 0.f, g);
       gate8<false>(k.gate_act, g, f, nullptr);
     } else {
 #pragma unroll
@@ -50,11 +51,11 @@ __global__ __launch_bounds__(MOST) void block_forward_kernel(BlockArgs a, int64_
   for (; r < r_end; r += ROWS) {
     const int64_t row = i * k.rows + r;
     float u[8], o[8];
-    get_row<TINY>(y, u, n);
-    get_row<TINY>(x, o, n);
+    reader.get(y, u);
+    reader.get(x, o);
     if (rows_gate) {
       float g[8];
-      get_row<TINY>(gate, g, n);
+      reader.get(gate, g);
       gate8<false>(k.gate_act, g, f, nullptr);
     }
     if (r + ROWS < r_end) fetch(r + ROWS);   // (on its way while this row is reduced)
@@ -86,8 +87,10 @@ void launch(const BlockArgs& a, hipStream_t s) {
   const int moved = (int)((a.n.pre != PBT_NORM_NONE ? 2 : 1) * sizeof(A) + (a.n.gate == PBT_GATE_ROWS ? sizeof(A) : 0) + 2 * sizeof(R));
   const int64_t per_slab = slab_rows(a.n, extra, moved, std::max(16 / (t.threads / 64), 1), 4096);
   const dim3 grid((unsigned)((a.n.rows + per_slab - 1) / per_slab), a.n.P), block(t.threads);
-  if (a.n.d < 8) hipLaunchKernelGGL((block_forward_kernel<A, R, 8, 256, true>), grid, block, 0, s, a, per_slab);
-  else if (t.T == 8) hipLaunchKernelGGL((block_forward_kernel<A, R, 8, 256, false>), grid, block, 0, s, a, per_slab);
+  if (ends_alone(a.n.d)) {
+    if (t.T == WIDE) hipLaunchKernelGGL((block_forward_kernel<A, R, WIDE, 1024, true>), grid, block, 0, s, a, per_slab);
+    else hipLaunchKernelGGL((block_forward_kernel<A, R, 8, 256, true>), grid, block, 0, s, a, per_slab);
+  } else if (t.T == 8) hipLaunchKernelGGL((block_forward_kernel<A, R, 8, 256, false>), grid, block, 0, s, a, per_slab);
   else if (t.T == 32) hipLaunchKernelGGL((block_forward_kernel<A, R, 32, 256, false>), grid, block, 0, s, a, per_slab);
   else if (t.T == 16) hipLaunchKernelGGL((block_forward_kernel<A, R, 16, 256, false>), grid, block, 0, s, a, per_slab);
   else if (t.T == 64) hipLaunchKernelGGL((block_forward_kernel<A, R, 64, 256, false>), grid, block, 0, s, a, per_slab);

@@ -105,8 +105,9 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 }
 // the factor of a member of norm n; 1: it stays as it is.  (Rounded to float once, like the norm that is handed out.)
 __device__ __forceinline__ float factor(double n, const float* max_norm) {
-  const double m = (double)*max_norm;
-  return n > m ? (float)(fmax(m, 0.0) / n) : 1.f;
+  double m = (double)*max_norm;
+  m = m < 0.0 ? 0.0 : m;   // (NaN stays: no comparison with it holds)
+  return n > m ? (float)(m / n) : 1.f;
 }
 
 // ---- small members: held in registers ----

@@ -91,10 +91,10 @@ def test_clip_tensors_of_one_flat_array_with_rows_at_any_address():
 
 
 def test_clip_values_at_the_ends_of_the_range():
-    """Squares that float32 cannot hold, zeros, infinities and NaN; bounds that are NaN or negative."""
+    """Squares that float32 cannot hold, zeros, infinities and NaN; bounds that are NaN or negative (of a zero gradient too)."""
     inf, nan = float("inf"), float("nan")
-    rows = torch.tensor([[3e38, -3e38, 1e38, 0], [1e-38, 1e-40, 0, 1e-45], [0, 0, 0, 0], [1, inf, -2, 3], [1, nan, 2, inf], [3, 4, 0, 0], [3, 4, 0, 0]], device="cuda")
-    bounds = torch.tensor([1.0, 1e-39, 1.0, 1.0, 1.0, nan, -1.0], device="cuda")
+    rows = torch.tensor([[3e38, -3e38, 1e38, 0], [1e-38, 1e-40, 0, 1e-45], [0, 0, 0, 0], [1, inf, -2, 3], [1, nan, 2, inf], [3, 4, 0, 0], [3, 4, 0, 0], [0, 0, 0, 0]], device="cuda")
+    bounds = torch.tensor([1.0, 1e-39, 1.0, 1.0, 1.0, nan, -1.0, -1.0], device="cuda")
     out = torch.empty_like(rows)
     norms = binding.GradClip([rows], [out])(bounds)
     want = np.sqrt((_cpu(rows) ** 2).sum(axis=1))
@@ -103,7 +103,7 @@ def test_clip_values_at_the_ends_of_the_range():
     o = _cpu(out)
     # the factor 1 / 4.4e38 is below the smallest normal float (1.2e-38): it keeps 2^-149 of absolute precision, 2^-150 / 2.3e-39 relative
     assert np.allclose(o[0], _cpu(rows)[0] / want[0], rtol=2.0 ** -150 / 2.2e-39 + 2 * U, atol=0)
-    assert o[2].tolist() == [0, 0, 0, 0] and o[5].tolist() == [3, 4, 0, 0] and o[6].tolist() == [0, 0, 0, 0]
+    assert o[2].tolist() == [0, 0, 0, 0] and o[5].tolist() == [3, 4, 0, 0] and o[6].tolist() == [0, 0, 0, 0] and o[7].tolist() == [0, 0, 0, 0]
     assert o[3][0] == 0 and o[3][2] == 0 and np.isnan(o[3][1])
     assert o[4][0] == 1 and np.isnan(o[4][1]) and np.isinf(o[4][3])
 
@@ -355,7 +355,7 @@ def _check_block(c, P, rows, d, post, pre, gate, act, dtype, res, alpha=0.9, bet
             _close(v[i], w_grads[k], (CHAIN + rows) * U * m[k], (k, i))
 
 
-SHAPES = [(1, 1, 1), (1, 1, 8), (2, 3, 5), (3, 70, 7), (2, 33, 64), (1, 65, 61), (2, 40, 200), (1, 9, 256), (1, 5, 128), (3, 7, 130), (1, 33, 512), (2, 9, 513), (1, 4, 1024), (1, 3, 1500), (1, 2, 2048), (2, 2, 4095), (1, 3, 5001), (1, 2, 8192), (2, 700, 24)]
+SHAPES = [(1, 1, 1), (1, 1, 8), (2, 3, 5), (3, 70, 7), (2, 33, 64), (1, 65, 61), (2, 40, 200), (1, 9, 256), (1, 5, 128), (3, 7, 130), (1, 33, 512), (2, 9, 513), (1, 4, 1024), (1, 3, 1500), (2, 5, 1025), (1, 4, 4609), (1, 2, 2048), (2, 2, 4095), (1, 3, 5001), (1, 2, 8192), (2, 700, 24)]
 
 
 @pytest.mark.parametrize("P,rows,d", SHAPES)
@@ -563,3 +563,28 @@ def test_block_norm_some_parameters_of_wide_rows(names):
     some = {k: torch.full_like(grads[k], 9.0) for k in names}
     dy2, dx2, _, _ = op.backward(c["y"], c["x"], c["params"], stats, c["dout"], c["dz"], grads=some)
     assert torch.equal(dy, dy2) and torch.equal(dx, dx2) and all(torch.equal(some[k], grads[k]) for k in names)
+
+
+@pytest.mark.parametrize("d", [5, 61, 513, 519, 1027, 4099, 5001])
+@pytest.mark.parametrize("post,pre", [("none", "rms"), ("layer", "none"), ("rms", "layer")])
+def test_block_norm_over_its_inputs_at_widths_that_end_anywhere(d, post, pre):
+    """out over x, z over y, dx over dout, dy over dz, where the lane at a row's end shares its eight elements with its neighbours: the same bits as apart."""
+    rows = 37
+    c = _case(1, rows, d, post, pre, "rows", "sigmoid", "bf16", "bf16")
+    op = binding.BlockNorm(d, post=post, pre=pre, gate="rows", act="sigmoid")
+    out, z, stats = op.forward(c["y"], c["x"], c["params"], gate=c["gate"])
+    dy, dx, dgate, grads = op.backward(c["y"], c["x"], c["params"], stats, c["dout"], c["dz"], gate=c["gate"])
+    y, x = c["y"].clone(), c["x"].clone()
+    _, _, stats2 = op.forward(y, x, c["params"], gate=c["gate"], out=x, z=y)
+    assert torch.equal(x, out) and torch.equal(stats, stats2) and (z is None or torch.equal(y, z))
+    dout, dz = c["dout"].clone(), None if c["dz"] is None else c["dz"].clone()
+    dy2, _, dgate2, grads2 = op.backward(c["y"], c["x"], c["params"], stats, dout, dz, gate=c["gate"], dy=dz, dx=dout)
+    assert torch.equal(dout, dx) and torch.equal(dy2, dy) and torch.equal(dgate, dgate2) and all(torch.equal(grads[k], grads2[k]) for k in grads)
+
+
+def test_rotary_of_one_groups_heads_twice_is_refused():
+    x = torch.zeros(4, 2, 8, device="cuda")
+    r = binding.Rotary(8)
+    for src, dst in (([x, x], None), ([x, x[:, :1]], None), ([x, x.clone()], [torch.empty_like(x), x])):
+        with pytest.raises(binding.PbtError):
+            r(src, dst)

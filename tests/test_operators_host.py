@@ -86,6 +86,20 @@ def test_rotary_apply_refusals(call):
     assert _apply(**call) == EINVAL
 
 
+def test_rotary_groups_that_meet_are_refused():
+    """The same heads twice, one group's dst over another's src or dst, halves of heads over one another.  (Adjacent heads of one projection in place are
+    what test_gpu_operators.py does.)"""
+    far = MEM + (1 << 30)
+    for a, b in (((MEM, MEM), (MEM, MEM)), ((MEM, far), (far, far)), ((MEM, far), (MEM + 1024, far + 512)), ((MEM, MEM), (MEM + 512, MEM + 512))):
+        assert _apply_two(a, b) == EINVAL and b"overlaps group" in binding.lib().pbt_last_error(None), (a, b)
+
+
+def _apply_two(a, b):
+    base = dict(src_row=1536, src_head=64, dst_row=1536, dst_head=64, heads=8, unused=0)
+    groups = (binding.PbtHeads * 2)(binding.PbtHeads(**base, d_src=a[0], d_dst=a[1]), binding.PbtHeads(**base, d_src=b[0], d_dst=b[1]))
+    return binding.lib().pbt_rotary_apply(C.byref(_settings()), MEM, groups, 2, 1, 10, 64, None, 0, 0, 0, 0, None)
+
+
 def test_rotary_of_no_rows_is_done():
     assert _apply(rows=0) == 0
 
