@@ -6,6 +6,7 @@ library's HIP kernels.  PyTorch supplies device memory (`torch.empty` on
 import of a symbol fails loudly; there is no fallback path.
 """
 import ctypes as C
+import functools
 import math
 import os
 
@@ -432,14 +433,22 @@ _I64x16, _I64x28 = C.c_int64 * 16, C.c_int64 * 28
 BLOCK_PARAMS = ("post_gain", "post_bias", "pre_gain", "pre_bias", "gate")
 
 
+@functools.lru_cache(None)
+def _stream_of():
+    """Device index -> handle of its current stream, without the Python object around it where torch offers that (2 of the 9 us of a small call)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(device, fn, *args):
     """fn(*args, stream) with the device's current stream; kernels are launched on the current device, so it is made current if it is not."""
     import torch
     if torch.cuda.current_device() == device.index:
-        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        rc = fn(*args, _stream_of()(device.index))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+            rc = fn(*args, _stream_of()(device.index))
     if rc != 0:
         raise PbtError(rc, lib().pbt_last_error(None).decode())
 
@@ -609,13 +618,14 @@ class BlockNorm:
         return known
 
     @staticmethod
-    def _rows(t, like, what):
+    def _rows(t, shape, dtype, device, what):
         """(address, pitch) of a matrix."""
         if t is None:
             return 0, 0
-        if t.shape != like.shape or t.dtype is not like.dtype or t.device != like.device:
-            raise ValueError("%s: shape, type and device of %s are wanted" % (what, tuple(like.shape)))
-        (n, d), (pitch, step) = t.shape, t.stride()
+        if t.shape != shape or t.dtype is not dtype or t.device != device:
+            raise ValueError("%s: a tensor %s, %s, on %s is wanted" % (what, tuple(shape), dtype, device))
+        pitch, step = t.stride()
+        n, d = shape
         if step != 1 and d > 1:
             raise ValueError("%s: a row's elements must be adjacent" % what)
         return t.data_ptr(), pitch if n > 1 else d
@@ -652,18 +662,21 @@ class BlockNorm:
         """Returns (out, z, stats); z is None with pre = "none", stats (float32 [rows, 4], for backward) with stats = False."""
         import torch
         s, _ = self._settings(y, x)
-        device = y.device
-        if device.type != "cuda" or x.device != device or x.shape != y.shape:
-            raise ValueError("y and x: device tensors of one shape, on one device")
+        device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
+        if device.type != "cuda":
+            raise ValueError("device tensors are wanted")
+        if gate is not None and not self._rows_gate:
+            raise ValueError("a gate's matrix goes with gate = \"rows\"")
         if out is None:
             out = torch.empty_like(x)
         if not self._pre:
             z = None
         elif z is None:
             z = torch.empty_like(y)
-        st = torch.empty((y.shape[0], 4), dtype=torch.float32, device=device) if stats else None
-        a = _I64x16(*self._rows(y, y, "y"), *self._rows(x, x, "x"), *self._rows(gate if self._rows_gate else None, y, "gate"), *self._rows(out, x, "out"),
-                    *self._rows(z, y, "z"), *self._params(params, device))
+        st = torch.empty((shape[0], 4), dtype=torch.float32, device=device) if stats else None
+        rows = self._rows
+        a = _I64x16(*rows(y, shape, ty, device, "y"), *rows(x, shape, tx, device, "x"), *rows(gate, shape, ty, device, "gate"),
+                    *rows(out, shape, tx, device, "out"), *rows(z, shape, ty, device, "z"), *self._params(params, device))
         at = C.addressof(a)
         _call(device, lib().pbt_block_norm_forward, C.byref(s), at, at + 16, at + 32, at + 80, at + 48, at + 64, 0 if st is None else st.data_ptr())
         return out, z, st
@@ -673,9 +686,9 @@ class BlockNorm:
         grads: dict of float32 [members, width] for the parameters in params (or the tensors given as `grads`, which are overwritten)."""
         import torch
         s, work_bytes = self._settings(y, x)
-        device = y.device
-        if device.type != "cuda" or x.device != device or x.shape != y.shape:
-            raise ValueError("y and x: device tensors of one shape, on one device")
+        device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
+        if device.type != "cuda":
+            raise ValueError("device tensors are wanted")
         if stats.shape != (y.shape[0], 4) or stats.dtype is not torch.float32 or not stats.is_contiguous() or stats.device != device:
             raise ValueError("stats: what forward returned")
         if dy is None:
@@ -683,15 +696,17 @@ class BlockNorm:
         if dx is None:
             dx = torch.empty_like(x)
         if not self._rows_gate:
-            gate = dgate = None
+            if gate is not None or dgate is not None:
+                raise ValueError("a gate's matrix goes with gate = \"rows\"")
         elif dgate is None:
             dgate = torch.empty_like(y)
         if grads is None:
             names = [k for k, t in (params or {}).items() if t is not None]
             grads = dict(zip(names, torch.empty((len(names), self.members, self.width), dtype=torch.float32, device=device).unbind(0)))
-        a = _I64x28(*self._rows(y, y, "y"), *self._rows(x, x, "x"), *self._rows(gate, y, "gate"), *self._rows(dout, x, "dout"),
-                    *self._rows(dz if self._pre else None, y, "dz"), *self._rows(dy, y, "dy"), *self._rows(dx, x, "dx"), *self._rows(dgate, y, "dgate"),
-                    *self._params(params, device), *self._params(grads, device))
+        rows = self._rows
+        a = _I64x28(*rows(y, shape, ty, device, "y"), *rows(x, shape, tx, device, "x"), *rows(gate, shape, ty, device, "gate"), *rows(dout, shape, tx, device, "dout"),
+                    *rows(dz if self._pre else None, shape, ty, device, "dz"), *rows(dy, shape, ty, device, "dy"), *rows(dx, shape, tx, device, "dx"),
+                    *rows(dgate, shape, ty, device, "dgate"), *self._params(params, device), *self._params(grads, device))
         at = C.addressof(a)
         work = torch.empty(work_bytes, dtype=torch.uint8, device=device)   # (of this call: calls on two streams do not meet in it)
         _call(device, lib().pbt_block_norm_backward, C.byref(s), at, at + 16, at + 32, at + 128, stats.data_ptr(), at + 48, at + 64, at + 80, at + 96, at + 112, at + 176,

@@ -81,7 +81,7 @@ struct Shape {
   int rows, heads;           // of a workgroup
   int head_blocks, row_blocks;   // blocks = head_blocks row_blocks
   int pair_units, units;     // of a head: units of pairs, then those of the part that is copied
-  uint32_t by_units, by_heads;
+  uint32_t by_units, by_heads, by_pitch;
 };
 struct Shapes { Shape g[4]; };
 
@@ -103,6 +103,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes
       grp = a.g[g];
     }
   const int pairs = a.rot / 2, head0 = (int)((uint32_t)block % (uint32_t)w.head_blocks) * w.heads, heads = min(w.heads, grp.heads - head0);
+  // Where results go elsewhere, a last unit that would not be whole starts earlier instead: what it shares with its neighbour both compute alike.  (In
+  // place one of the two could read what the other has written.)
+  const bool apart = grp.d_src != grp.d_dst, pairs_back = apart && pairs >= PV, copy_back = a.width - a.rot >= V;
   struct Item { const T* src; T* dst; Vec16 x, y; int lds, n; };   // n: pairs (-elements where the unit is copied); lds: the unit's first angle
   for (int64_t row0 = (int64_t)((uint32_t)block / (uint32_t)w.head_blocks) * w.rows; row0 < a.rows; row0 += (int64_t)w.row_blocks * w.rows) {
     const int rows = (int)min((int64_t)w.rows, a.rows - row0);
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes
       it.src = static_cast<const T*>(grp.d_src) + (row0 + r) * grp.src_row + (head0 + h) * grp.src_head;
       it.dst = static_cast<T*>(grp.d_dst) + (row0 + r) * grp.dst_row + (head0 + h) * grp.dst_head;
       if (u < w.pair_units) {
-        const int j = u * PV;
+        const int j = pairs_back ? min(u * PV, pairs - PV) : u * PV;
         it.n = min(PV, pairs - j);
         it.lds = r * pitch + j;
         if (LAYOUT == PBT_ROTARY_HALF) {
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes
           it.x = Unit<T>::load(it.src, 2 * it.n);
         }
       } else {
-        const int e = a.rot + (u - w.pair_units) * V;
+        const int from = a.rot + (u - w.pair_units) * V, e = copy_back ? min(from, a.width - V) : from;
         it.src += e;
         it.dst += e;
         it.n = -min(V, a.width - e);
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes
     };
     Item it = fetch(threadIdx.x);   // (on its way while the angles are formed)
     for (int k = threadIdx.x; k < rows * pitch; k += 256) {
-      const int r = k / pitch, j = k - r * pitch;
+      const int r = quotient(k, w.by_pitch), j = k - r * pitch;
       if (j < pairs) {
         const float2 cs = turn((double)position(a, row0 + r) * a.turns[j]);
         table[k] = cs.x * a.gain;
@@ -229,6 +232,7 @@ hipError_t launch(RotaryArgs a, hipStream_t s) {
     w.rows = (int)rows;
     w.by_units = magic(w.units);
     w.by_heads = magic(w.heads);
+    w.by_pitch = magic(pitch);
     // (a grid holds 2^32 threads: the workgroups of a group take several blocks of rows where there would be more than 2^21 of them)
     w.row_blocks = (int)std::min((a.rows + rows - 1) / rows, std::max<int64_t>((1 << 21) / w.head_blocks, 1));
     w.blocks = (int64_t)w.row_blocks * w.head_blocks;

@@ -588,3 +588,41 @@ def test_rotary_of_one_groups_heads_twice_is_refused():
     for src, dst in (([x, x], None), ([x, x[:, :1]], None), ([x, x.clone()], [torch.empty_like(x), x])):
         with pytest.raises(binding.PbtError):
             r(src, dst)
+
+
+def test_block_norm_rows_far_apart():
+    """Rows 2^31 bytes from one another, forward and backward; nothing between them is written."""
+    P, rows, d = 1, 3, 72
+    kw = dict(post="rms", pre="layer", gate="rows", act="sigmoid")
+    c = _case(P, rows, d, dtype="bf16", res="bf16", **kw)
+    op = binding.BlockNorm(d, **kw)
+    out, z, stats = op.forward(c["y"], c["x"], c["params"], gate=c["gate"])
+    dy, dx, dgate, _ = op.backward(c["y"], c["x"], c["params"], stats, c["dout"], c["dz"], gate=c["gate"])
+    big = torch.zeros(rows, 1 << 30, dtype=torch.bfloat16, device="cuda")
+    at = iter(range(0, 9 * 128, 128))
+
+    def far(t=None):
+        k = (1 << 30) - 2000 + next(at)
+        v = big[:, k:k + d]
+        if t is not None:
+            v.copy_(t)
+        return v
+
+    y, x, gate = far(c["y"]), far(c["x"]), far(c["gate"])
+    out2, z2, stats2 = op.forward(y, x, c["params"], gate=gate, out=far(), z=far())
+    dout, dz = far(c["dout"]), far(c["dz"])
+    dy2, dx2, dgate2, _ = op.backward(y, x, c["params"], stats2, dout, dz, gate=gate, dy=dz, dx=dout, dgate=far())
+    for a, b in ((out, out2), (z, z2), (stats, stats2), (dy, dy2), (dx, dx2), (dgate, dgate2)):
+        assert torch.equal(a, b)
+    assert not big[:, :(1 << 30) - 2000].any() and not big[:, -600:].any()
+
+
+def test_block_norm_gate_matrix_needs_its_kind():
+    y = torch.zeros(2, 16, device="cuda")
+    op = binding.BlockNorm(16)
+    with pytest.raises(ValueError):
+        op.forward(y, y, gate=y)
+    stats = op.forward(y, y)[2]
+    for kw in (dict(gate=y), dict(dgate=y)):
+        with pytest.raises(ValueError):
+            op.backward(y, y, {}, stats, y, y, **kw)
