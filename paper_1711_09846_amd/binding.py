@@ -497,7 +497,7 @@ class GradClip:
         for e, g, o in zip(table, grads, outs):
             if g.dim() < 1 or g.shape[0] != self.P or o.shape != g.shape or o.dtype != g.dtype:
                 raise ValueError("tensors [P, ...] with the same P are wanted, and outs of the same shapes and types")
-            if g.numel() and not (g[0].is_contiguous() and o[0].is_contiguous()):
+            if g.numel() and not all(t.is_contiguous() or t[0].is_contiguous() for t in (g, o)):
                 raise ValueError("a member's part of a tensor must be contiguous")
             e.d_src, e.d_dst, e.dtype = g.data_ptr(), o.data_ptr(), _dtype_code(g)
             e.len = g.numel() // self.P if self.P else 0

@@ -4,6 +4,8 @@
 // u and out are formed again from y, x and the gate.  dz hat, dz, v hat, v (and dgate for a gate vector) are summed over a slab's rows in registers; the
 // slabs' sums go to `part`, and a second launch adds them in slab order.  The parameters wait in LDS: a compute unit gets some eight bytes a cycle from memory
 // and 128 from LDS, registers are what limits how many rows are on their way.
+// Bound by memory: 16 x 4096 rows of 512 with a gate a row and the stream in fp32, 738 MB: 150 us (4.9 TB/s); 16384 rows of 2048: 131 (4.6); 8191 rows of 5001:
+// 115 (4.3).  The second launch: 4 to 10 us.
 #include <algorithm>
 #include <type_traits>
 

@@ -1,4 +1,7 @@
 // Block norms, forward: u = N_post(y), out = alpha x + beta a(gate) u, z = N_pre(out) in one pass over y, x and the gate.
+// Bound by memory: 16 x 4096 rows of 512 bf16 with a gate vector, 268 MB: 53 to 59 us; with a gate a row and the stream in fp32, 470 MB: 88 (5.3 TB/s); 16384 rows of
+// 2048: 84 (4.8).  Rows of ten wavefronts leave two workgroups a compute unit, and three barriers a row show: 8191 rows of 5001: 94 us (3.5 TB/s).  4 rows of
+// 2048: 3.4 us.
 #include <algorithm>
 #include <type_traits>
 

@@ -109,7 +109,7 @@ hipError_t rotary_plan(const RotaryFrequencies& f, int n, double* table, hipStre
 void rotary_frequencies(const pbt_rotary& r, RotaryFrequencies* f);
 struct RotaryArgs {
   pbt_heads g[4];
-  int n_groups, heads;      // heads of all groups
+  int n_groups;
   int64_t rows;
   int width, rot;
   const void* pos;

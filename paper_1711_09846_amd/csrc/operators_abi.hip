@@ -212,7 +212,7 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
   RotaryArgs a;
   std::memset(&a, 0, sizeof a);
   for (int k = 0; k < n_groups; ++k) a.g[k] = h_groups[k];
-  a.n_groups = n_groups; a.heads = (int)heads;
+  a.n_groups = n_groups;
   a.rows = rows; a.width = width; a.rot = r->rot_dim;
   a.pos = d_positions; a.pos64 = position_bytes == 8;
   a.start = start; a.period = period;

@@ -117,7 +117,7 @@ pbt_status turn_heads(const Ctx& x, bf16_t* qkv, int backward) {
   const Dim& D = x.D;
   RotaryArgs a{};
   a.g[0] = pbt_heads{qkv, qkv, 3 * D.d, D.dh, 3 * D.d, D.dh, 2 * D.H, 0};
-  a.n_groups = 1; a.heads = 2 * D.H;
+  a.n_groups = 1;
   a.rows = (int64_t)x.P * x.n; a.width = D.dh; a.rot = t.opt.rot.rot_dim;
   a.period = D.S;   // (rows are whole sequences)
   a.gain = (float)t.opt.rot.gain; a.sign = backward ? -1.f : 1.f;
