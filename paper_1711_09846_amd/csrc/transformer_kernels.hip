@@ -37,9 +37,10 @@ __device__ __forceinline__ void store8(bf16_t* p, const float* v) {
 }
 
 // ---- embeddings ------------------------------------------------------------------------------
-// h[i][b][s][:] = tok[token] + pos[s] (pos_off < 0: without positions); tokens are drawn here: sequence b of member i is pool row
+// h[i][b][s][:] = tok[token] + pos[s] (POS: with positions, by pos_off >= 0; a kernel each, a branch between the loads costs 3 us); tokens are drawn here: sequence b of member i is pool row
 // floor(x * n_pool / 2^32), x from Philox domain 1; also copies the targets and bumps t.
 // A wavefront per position, eight elements (16 bytes) per lane and pass: 65536 rows of 512 in 35 us (47 with 2-byte accesses).
+template <bool POS>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(const int32_t* __restrict__ pool, int n_pool, int S, int B, int d, int V,
                                                         const bf16_t* __restrict__ W16, int64_t stride, int64_t tok_off,
                                                         int64_t pos_off, uint32_t c0, uint32_t k0, uint32_t k1, int draw,
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const int32_t* __restric
   for (int c = lane * 8; c < d; c += 512) {
     float v[8], w[8];
     load8(te + c, v);
-    if (pos_off >= 0) {
+    if (POS) {
       load8(pe + c, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += w[e];
@@ -75,7 +76,7 @@ hipError_t embed_fwd(const int32_t* pool, int n_pool, int S, int B, int d, int V
                      int64_t tok_off, int64_t pos_off, uint32_t c0, uint64_t seed, int draw, bf16_t* h, int32_t* tokens,
                      int32_t* targets, int32_t* t, hipStream_t s) {
   if (d % 8 || stride % 8 || tok_off % 8 || (pos_off >= 0 && pos_off % 8)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(embed_fwd_kernel, dim3((unsigned)((B * S + 3) / 4), P), dim3(256), 0, s, pool, n_pool, S, B, d, V, W16, stride, tok_off, pos_off, c0,
+  hipLaunchKernelGGL(pos_off >= 0 ? embed_fwd_kernel<true> : embed_fwd_kernel<false>, dim3((unsigned)((B * S + 3) / 4), P), dim3(256), 0, s, pool, n_pool, S, B, d, V, W16, stride, tok_off, pos_off, c0,
                      (uint32_t)seed, (uint32_t)(seed >> 32), draw, h, tokens, targets, t);
   return hipGetLastError();
 }
