@@ -127,12 +127,14 @@ hipError_t row_reduce(const float* rowval, int64_t srow, int P, int rows, float 
 // pass, 1820 -> 1876 / 1855 us on the transformer).
 constexpr int OPT_VEC_PER_THREAD = 1;
 
-// SCALED: gradients times their member's factor.  (A kernel of its own: a branch between the loads makes the later ones wait, 1756 -> 1786 us.)
+// SCALED: gradients times their member's factor.  (A kernel of its own: a branch between the loads makes the later ones wait, 1756 -> 1786 us.  The factor is read
+// with the other scalars: 1764 us behind the loads, 1708 so.)
 template <int OPT, bool SCALED>
 __global__ __launch_bounds__(256) void optimizer_kernel(OptArgs a) {
   const int i = blockIdx.y;
   const OptHyper hy{a.H, a.t, a.n_hyper, a.col_lr, a.col_beta1, a.col_wd, a.c0, a.c1, a.c2, a.c3, a.t_mul, a.t_add};
   const OptScalars sc = opt_scalars<OPT>(hy, i);
+  const float scale = SCALED ? a.g_scale[i] : 1.f;
 #pragma unroll
   for (int u = 0; u < OPT_VEC_PER_THREAD; ++u) {
     // vector index over the concatenation of the ranges
@@ -150,10 +152,7 @@ __global__ __launch_bounds__(256) void optimizer_kernel(OptArgs a) {
     float4 s0 = stream_load(a.S0 + o);
     float4 s1 = make_float4(0.f, 0.f, 0.f, 0.f);
     if (OPT == OPT_ADAM) s1 = stream_load(a.S1 + o);
-    if (SCALED) {
-      const float c = a.g_scale[i];
-      g = make_float4(g.x * c, g.y * c, g.z * c, g.w * c);
-    }
+    if (SCALED) g = make_float4(g.x * scale, g.y * scale, g.z * scale, g.w * scale);
     float* wp = reinterpret_cast<float*>(&w);
     const float* gp = reinterpret_cast<const float*>(&g);
     float* s0p = reinterpret_cast<float*>(&s0);
