@@ -6,10 +6,10 @@
 // fewer workgroups fit a compute unit (131072 rows: 812 us).
 // 16 of 24 heads of 64 in 65536 rows, bf16: 58 us, a copy of the same heads 49; 40 of 60 heads of 128 in 131072 rows: 495 us (5.4 TB/s), a copy 472; fp32 rows
 // of 5 heads of 84 with 42 turned, 9973 of them: 9.7 us, a copy 6.8; 16 rows: 3.1.
-#include <algorithm>
 #include <cmath>
 
 #include "operators.h"
+#include "operators_choose.h"
 
 namespace pbt {
 namespace {
@@ -79,23 +79,14 @@ __device__ __forceinline__ void put(T* p, const Vec16& a, int n) {
 // n / d for n d < 2^32, by a product with ceil(2^32 / d) (d = 1: 0)
 __device__ __forceinline__ int quotient(int n, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)n, magic) : n; }
 
-struct Shape {
-  int64_t blocks;            // workgroups of the group of heads
-  int rows, heads;           // of a workgroup
-  int head_blocks, row_blocks;   // blocks = head_blocks row_blocks
-  int pair_units, units;     // of a head: units of pairs, then those of the part that is copied
-  uint32_t by_units, by_heads, by_pitch;
-};
-struct Shapes { Shape g[4]; };
-
 // NT: stores that no cache keeps
 template <class T, int LAYOUT, bool NT>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes, int pitch) {
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, RotaryShapes shapes, int pitch) {
   extern __shared__ float table[];   // [rows][pitch] cosines, then sines
   constexpr int V = Unit<T>::V;
-  constexpr int PV = LAYOUT == PBT_ROTARY_HALF ? V : V / 2;   // pairs of a unit
+  constexpr int PV = rotary_unit_pairs(V, LAYOUT == PBT_ROTARY_HALF);
   // the workgroup's group of heads (one after the other in the grid)
-  Shape w = shapes.g[0];
+  RotaryShape w = shapes.g[0];
   pbt_heads grp = a.g[0];
   int64_t block = blockIdx.x;
 #pragma unroll
@@ -202,52 +193,21 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, Shapes shapes
   }
 }
 
-uint32_t magic(int d) { return d <= 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
-
 template <class T, int LAYOUT>
 hipError_t launch(RotaryArgs a, hipStream_t s) {
   if (a.period >= a.rows) a.period = 0;   // (the rows end before it does)
-  constexpr int V = Unit<T>::V, PV = LAYOUT == PBT_ROTARY_HALF ? V : V / 2;
-  const int pairs = a.rot / 2, pitch = (pairs + 3) / 4 * 4;
-  Shapes shapes{};
-  int64_t total = 0;
-  int most_rows = 1;
+  RotaryCall call{Unit<T>::V, LAYOUT == PBT_ROTARY_HALF, a.rot, a.width, a.rows, a.n_groups, {}, {}};
   for (int g = 0; g < a.n_groups; ++g) {
-    Shape& w = shapes.g[g];
-    w.pair_units = (pairs + PV - 1) / PV;
-    w.units = w.pair_units + (a.g[g].d_src == a.g[g].d_dst ? 0 : (a.width - a.rot + V - 1) / V);
-    w.heads = std::min(std::max(2048 / w.units, 1), (int)a.g[g].heads);
-    w.head_blocks = (a.g[g].heads + w.heads - 1) / w.heads;
-    // A table in LDS serves few rows: the first number of them whose units fill nine tenths of the workgroup's last sweep (else the one that does best), while
-    // four workgroups are left for every compute unit and the table takes at most 16 KB.
-    const int per_row = w.heads * w.units;
-    int64_t limit = std::min<int64_t>(std::min<int64_t>(2048 / pitch, 2048 / per_row + 1), a.rows * w.head_blocks / 1024);
-    int64_t rows = 1;
-    double best = 0.0;
-    for (int64_t r = 1; r <= std::max<int64_t>(limit, 1) && best < 0.9; ++r) {
-      const int64_t n = r * per_row;
-      const double used = (double)n / (double)((n + 255) / 256 * 256);
-      if (used > best) {
-        best = used;
-        rows = r;
-      }
-    }
-    w.rows = (int)rows;
-    w.by_units = magic(w.units);
-    w.by_heads = magic(w.heads);
-    w.by_pitch = magic(pitch);
-    // (a grid holds 2^32 threads: the workgroups of a group take several blocks of rows where there would be more than 2^21 of them)
-    w.row_blocks = (int)std::min((a.rows + rows - 1) / rows, std::max<int64_t>((1 << 21) / w.head_blocks, 1));
-    w.blocks = (int64_t)w.row_blocks * w.head_blocks;
-    total += w.blocks;
-    most_rows = std::max(most_rows, w.rows);
+    call.heads[g] = a.g[g].heads;
+    call.apart[g] = a.g[g].d_src != a.g[g].d_dst;
   }
-  const size_t lds = (size_t)2 * most_rows * pitch * sizeof(float);
+  const RotaryCut cut = rotary_cut(call);
+  const size_t lds = (size_t)cut.table * sizeof(float);
   int64_t bytes = 0;
   for (int g = 0; g < a.n_groups; ++g) bytes += a.rows * a.g[g].heads * a.width * (int64_t)sizeof(T);
   // (131072 rows, 1.3 GB: 495 us past the caches, 514 through them; 65536 rows, 134 MB: 63 and 58)
-  if (bytes > LAST_CACHE) hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, true>), dim3((unsigned)total), dim3(256), lds, s, a, shapes, pitch);
-  else hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, false>), dim3((unsigned)total), dim3(256), lds, s, a, shapes, pitch);
+  if (bytes > LAST_CACHE) hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, true>), dim3((unsigned)cut.blocks), dim3(256), lds, s, a, cut.shapes, cut.pitch);
+  else hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, false>), dim3((unsigned)cut.blocks), dim3(256), lds, s, a, cut.shapes, cut.pitch);
   return hipGetLastError();
 }
 
