@@ -535,7 +535,7 @@ def rotary_settings(rot_dim, base=10000.0, layout="half", scaling="none", factor
 class Rotary:
     """Rotary positions on heads (pbt_rotary_plan, pbt_rotary_apply): rot_dim, base, layout ("half", "interleaved"), scaling ("none",
     "linear", "base", "ramp" with factor, and for "ramp" trained, low, high) and gain as in include/pbt.h.  Making one writes the table of frequencies and
-    waits for it, so that it can be used on any stream afterwards."""
+    waits for it, so that it can be used on any stream afterwards; a captured graph reads the table when it is replayed and keeps nothing alive."""
 
     def __init__(self, rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained=0.0, low=1.0, high=32.0, gain=1.0, device="cuda:0"):
         import torch
@@ -545,7 +545,9 @@ class Rotary:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.table = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64, device=self.device)
         _call(self.device, lib().pbt_rotary_plan, C.byref(self.settings), self.table.data_ptr(), self.table.numel() * 8)
-        torch.cuda.current_stream(self.device).synchronize()
+        stream = torch.cuda.current_stream(self.device)
+        stream.synchronize()
+        self._stream = stream.cuda_stream
 
     def __call__(self, src, dst=None, positions=None, start=0, period=0, backward=False):
         """src: tensor [rows, heads, width] with adjacent elements, or up to four of them (query and key heads); dst: the same, None: in place.
@@ -575,6 +577,8 @@ class Rotary:
             if positions.shape != (first.shape[0],) or positions.dtype not in (torch.int32, torch.int64) or not positions.is_contiguous() or positions.device != self.device:
                 raise ValueError("positions: a contiguous int32 or int64 tensor [rows] on the table's device")
             pos, size = positions.data_ptr(), positions.element_size()
+        if _stream_of()(self.device.index) != self._stream:
+            self.table.record_stream(torch.cuda.current_stream(self.device))   # (the table's memory is that stream's: not given away before this one is done)
         _call(self.device, lib().pbt_rotary_apply, C.byref(self.settings), self.table.data_ptr(), groups, len(srcs), _dtype_code(first), first.shape[0], first.shape[2],
               pos, size, start, period, int(bool(backward)))
         return dst

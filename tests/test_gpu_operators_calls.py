@@ -1,0 +1,38 @@
+"""Calls of the operators that their documentation allows, on streams, on memory that is shared or laid out otherwise, and those that are refused."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as oo
+from paper_1711_09846_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _gen(seed=0):
+    return torch.Generator().manual_seed(seed)
+
+
+def _normal(g, *shape, scale=1.0, dtype=torch.float32):
+    return (torch.randn(*shape, generator=g) * scale).to(dtype).cuda()
+
+
+def test_rotary_dropped_while_a_call_on_another_stream_is_pending():
+    """The table's memory is not given away before that call has read it."""
+    x = _normal(_gen(1), 64, 2, 64)
+    want = binding.Rotary(64)(x, torch.empty_like(x), start=5)
+    out = torch.empty_like(x)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    r = binding.Rotary(64)
+    table = r.table.data_ptr()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)      # (some 50 ms)
+        r(x, out, start=5)
+    del r
+    others = [torch.zeros(32, dtype=torch.float64, device="cuda") for _ in range(64)]
+    assert not side.query() and table not in [t.data_ptr() for t in others]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
