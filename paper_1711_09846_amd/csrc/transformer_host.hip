@@ -493,6 +493,12 @@ pbt_status tf_step(pbt_handle* h, const int32_t* pool, uint32_t step, hipStream_
   OptArgs oa{h->st<float>(p.o_w32), h->st<float>(p.o_opt0), h->st<float>(p.o_opt1), h->st<bf16_t>(p.o_w16), x.G, 0, x.S_,
              h->st<float>(p.o_hyper), h->st<int32_t>(p.o_t), x.S_, x.P, c.n_hyper, PBT_OPT_ADAM, p.col_lr, -1, -1,
              c.opt_const[0], c.opt_const[1], c.opt_const[2], c.opt_const[3]};
+  if (!t.opt.learned_positions) {   // (its gradient is zero, but weight decay and moments that were set would move the table)
+    oa.count = t.pos;
+    oa.n_extra = 1;
+    oa.xbegin[0] = p.lay.seg_off[2];
+    oa.xcount[0] = x.S_ - p.lay.seg_off[2];
+  }
   TF_TRY(clip_step(h, &oa, s));
   PBT_LAUNCH(h, PBT_K_OPTIMIZER, s, optimizer_step(oa, s));
   return PBT_OK;

@@ -1,0 +1,47 @@
+"""What options of the population step leave alone, whatever the rest of the configuration is."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1711_09846_amd import binding, workloads as W
+from tests.test_gpu_transformer import _reduced
+
+pytestmark = pytest.mark.gpu
+
+H2 = [[1e-3, 0.0, 0.0], [5e-4, 0.3, 0.05]]
+
+
+def _population(wl, H, opt_const=None):
+    pop = binding.Population(binding.make_config(wl if opt_const is None else wl.replace(opt_const=opt_const), W.POPULATION_SEED), tf_options=binding.make_tf_options(wl))
+    pop.set(binding.ARR_W32, np.stack([binding.pack_segments(pop.layout, a) for a in W.initial_transformer_weights(wl, wl.P, 5)]))
+    pop.set(binding.ARR_HYPER, np.asarray(H, dtype=np.float32))
+    return pop, [torch.from_numpy(W.zipf_bigram_sequences(wl)[0]).cuda()]
+
+
+@pytest.mark.parametrize("clip", [False, True])
+def test_unused_position_table_under_weight_decay_and_with_moments(clip):
+    """Without learned positions the table, its moments and its bf16 copy stay as they were set; every other array is updated."""
+    wl = _reduced(P=2, tf_options=dict(learned_positions=False, rotary=dict(rot_dim=16)))
+    H = H2
+    if clip:
+        wl = wl.replace(roles=wl.roles + [W.ROLE_CLIP_NORM], h_max=wl.h_max + [float("inf")], priors=wl.priors + [("log", 0.05, 5.0)])
+        H = [h + [0.1] for h in H2]
+    pop, pool = _population(wl, H, dict(wl.opt_const, wd=0.1))
+    lay = pop.layout
+    table = np.s_[:, lay.seg_off[1]:lay.seg_off[1] + lay.seg_len[1]]
+    rng = np.random.default_rng(3)
+    for which in (binding.ARR_OPT0, binding.ARR_OPT1):
+        m = pop.get(which)
+        m[table] = np.abs(rng.standard_normal(m[table].shape)).astype(np.float32)
+        pop.set(which, m)
+    arrays = (binding.ARR_W32, binding.ARR_OPT0, binding.ARR_OPT1, binding.ARR_W16)
+    before = {k: pop.get(k) for k in arrays}
+    for s in range(2):
+        pop.step(pool, s)
+    after = {k: pop.get(k) for k in arrays}
+    for k in arrays:
+        assert after[k][table].tobytes() == before[k][table].tobytes(), k
+    used = [j for j in range(lay.n_seg) if j != 1]
+    for j in used:
+        part = np.s_[:, lay.seg_off[j]:lay.seg_off[j] + lay.seg_len[j]]
+        assert (after[binding.ARR_OPT1][part] != before[binding.ARR_OPT1][part]).any(), j
