@@ -378,7 +378,7 @@ pbt_status pbt_batched_gemm_bf16(const void* d_a, int64_t lda, int64_t stride_a,
  *   norm_i = sqrt(sum over tensors and elements of g^2),   g <- g max_i / norm_i  where norm_i > max_i.
  * h_grads[k]: [P][len] elements, members src_stride (dst_stride) apart; dst may be src (with the same stride: clipped in
  * place), otherwise the two do not overlap and members below their bound are copied; no dst shares
- * elements with another tensor.  The largest norm of member i is read on the
+ * elements with another tensor (PBT_EINVAL: looked at in every call that clips).  The largest norm of member i is read on the
  * device, d_max_norm[i * max_norm_stride] (so a column of PBT_ARR_HYPER serves; a stride of 0: one bound for all);
  * NULL: norms only, dst is not looked at.  d_norm (float[P], may be NULL) receives the norm before clipping.
  * Squares are summed in double, in a fixed order: no finite gradient overflows or vanishes.  A member with a NaN has norm NaN and is not

@@ -482,7 +482,8 @@ class GradClip:
     """Gradient norms and clipping of P members over a list of tensors (pbt_clip_gradients).
 
     grads: tensors [P, ...], float32 or bfloat16, each member's part contiguous; outs: where the clipped gradients go (tensors of the same shapes
-    and types), None: clipped in place.  The tensors are kept, as an optimiser keeps its parameters.  A tensor may be listed once only.
+    and types), None: clipped in place.  The tensors are kept, as an optimiser keeps its parameters.  A tensor may be listed once only, and where
+    one's clipped gradient goes is no part of another.
     Calling it computes the norms [P] (float32) and, with max_norm (float32 tensor [P], any stride, or of one element for all members),
     scales every member whose norm is larger.  Without max_norm only the norms are computed."""
 

@@ -1,9 +1,12 @@
 // C ABI of the operators that need no handle: arguments are checked here, on the host, before anything is launched.
 #include <cmath>
 #include <cstring>
+#include <memory>
+#include <new>
 
 #include "handle.h"
 #include "operators.h"
+#include "operators_apart.h"
 
 using namespace pbt;
 
@@ -66,6 +69,28 @@ pbt_status check_grads(const pbt_grad* g, int n, int P, bool clip) {
       }
     }
   }
+  return PBT_OK;
+}
+
+// What a clipping call writes is apart from everything else that it touches (a tensor's own src and dst have been looked at).
+pbt_status check_grads_apart(const pbt_grad* g, int n, int P) {
+  constexpr int FEW = 128;
+  Region few[FEW];
+  std::unique_ptr<Region[]> many;
+  Region* r = few;
+  if (2 * (int64_t)n > FEW) {
+    many.reset(new (std::nothrow) Region[2 * (size_t)n]);
+    if (!(r = many.get())) return fail(nullptr, PBT_ENOMEM, "out of host memory");
+  }
+  int m = 0;
+  for (int k = 0; k < n; ++k) {
+    if (g[k].len == 0) continue;
+    const int64_t e = (int64_t)elem_bytes(g[k].dtype);
+    r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_dst), g[k].len * e, g[k].dst_stride * e, P, true, k};
+    if (g[k].d_src != g[k].d_dst) r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_src), g[k].len * e, g[k].src_stride * e, P, false, k};
+  }
+  int x, y;
+  if (find_meeting(r, m, &x, &y)) return fail(nullptr, PBT_EINVAL, "dst of one of the tensors %d and %d overlaps the other", std::min(x, y), std::max(x, y));
   return PBT_OK;
 }
 
@@ -156,6 +181,7 @@ pbt_status pbt_clip_gradients(const pbt_grad* h_grads, int32_t n_grads, int32_t 
   const size_t need = clip_work_bytes(h_grads, n_grads, P);
   if (!d_work || !aligned(d_work, 8)) return fail(nullptr, PBT_EINVAL, "work is NULL or not 8-byte aligned");
   if (work_bytes < need) return fail(nullptr, PBT_ENOMEM, "working memory: %zu bytes given, %zu needed", work_bytes, need);
+  if (d_max_norm) TRY(check_grads_apart(h_grads, n_grads, P));
   const hipError_t e = clip_gradients(h_grads, n_grads, P, d_max_norm, max_norm_stride, d_norm, d_work, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return fail(nullptr, PBT_EDEVICE, "clipping failed to launch: %s", hipGetErrorString(e));
   return PBT_OK;

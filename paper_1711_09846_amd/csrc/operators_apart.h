@@ -1,0 +1,89 @@
+// Whether the pieces of memory that a call reads and writes are apart: host code, for the entry points' checks of arguments.
+#pragma once
+#include <algorithm>
+#include <cstdint>
+
+namespace pbt {
+
+// `count` pieces of `bytes` bytes, `stride` bytes apart (stride >= bytes where there are several); what: whose they are, for the caller's message
+struct Region {
+  uintptr_t at;
+  int64_t bytes, stride, count;
+  bool written;
+  int what;
+  int64_t place = 0;   // (find_meeting's own)
+};
+inline int64_t region_span(const Region& r) { return r.bytes <= 0 || r.count <= 0 ? 0 : (r.count - 1) * r.stride + r.bytes; }
+
+// No byte of `a` is one of `b`.  Exact, but for two of different strides with thousands of pieces each, which are not looked at piece by piece where
+// they mix: those count as meeting.
+inline bool regions_apart(const Region& a, const Region& b) {
+  const int64_t sa = region_span(a), sb = region_span(b);
+  if (sa == 0 || sb == 0) return true;
+  if (a.at >= b.at + (uintptr_t)sb || b.at >= a.at + (uintptr_t)sa) return true;
+  if (a.count > 1 && b.count > 1 && a.stride == b.stride) {   // (the spans meet, so that some piece of one lies between two of the other or on one)
+    const int64_t p = a.stride, d = (int64_t)(b.at - a.at), m = ((d % p) + p) % p;
+    return m >= a.bytes && p - m >= b.bytes;
+  }
+  if (a.count > 1 && b.count > 1 && a.count + b.count > 8192) return false;
+  // piece by piece, from the first of each that can reach the other
+  int64_t i = 0, j = 0;
+  if (a.count > 1 && b.at > a.at) i = std::min<int64_t>((int64_t)(b.at - a.at) / a.stride, a.count - 1);
+  if (b.count > 1 && a.at > b.at) j = std::min<int64_t>((int64_t)(a.at - b.at) / b.stride, b.count - 1);
+  while (i < a.count && j < b.count) {
+    const uintptr_t x = a.at + (uintptr_t)(i * a.stride), y = b.at + (uintptr_t)(j * b.stride);
+    const uintptr_t xe = x + (uintptr_t)a.bytes, ye = y + (uintptr_t)b.bytes;
+    if (x < ye && y < xe) return false;
+    if (xe <= ye) ++i;
+    else ++j;
+  }
+  return true;
+}
+
+// The first pair of regions found that meet, one of them written, to *x and *y; false: there is none.  `r` is put in order of addresses.  Regions whose spans
+// meet are looked at together: where all are rows of one stride (a flat array's columns) by their places in a row, else pair by pair.
+inline bool find_meeting(Region* r, int n, int* x, int* y) {
+  const auto by_address = [](const Region& a, const Region& b) { return a.at < b.at; };
+  if (!std::is_sorted(r, r + n, by_address)) std::sort(r, r + n, by_address);
+  for (int lo = 0; lo < n;) {
+    uintptr_t end = r[lo].at + (uintptr_t)region_span(r[lo]);
+    bool rows = r[lo].count > 1;
+    int hi = lo + 1;
+    for (; hi < n && r[hi].at < end; ++hi) {
+      end = std::max(end, r[hi].at + (uintptr_t)region_span(r[hi]));
+      rows = rows && r[hi].count > 1 && r[hi].stride == r[lo].stride;
+    }
+    if (hi - lo > 1) {
+      bool clear = false;
+      if (rows && hi - lo > 8) {
+        // places in a row, twice around: what starts before the end of an earlier one meets it (or would, if their spans did: pairs decide then)
+        const uintptr_t base = r[lo].at;
+        const int64_t p = r[lo].stride;
+        const auto by_place = [](const Region& a, const Region& b) { return a.place < b.place; };
+        for (int k = lo; k < hi; ++k) r[k].place = (int64_t)(r[k].at - base) < p ? (int64_t)(r[k].at - base) : (int64_t)(r[k].at - base) % p;
+        if (!std::is_sorted(r + lo, r + hi, by_place)) std::sort(r + lo, r + hi, by_place);
+        clear = true;
+        int64_t read = 0, wrote = 0;   // ends of what came before
+        for (int lap = 0; lap < 2 && clear; ++lap)
+          for (int k = lo; k < hi && clear; ++k) {
+            if (region_span(r[k]) == 0) continue;
+            const int64_t at = r[k].place + lap * p;
+            clear = at >= wrote && (!r[k].written || at >= read);
+            int64_t& e = r[k].written ? wrote : read;
+            e = std::max(e, at + r[k].bytes);
+          }
+      }
+      for (int i = lo; i < hi && !clear; ++i)
+        for (int j = i + 1; j < hi; ++j)
+          if ((r[i].written || r[j].written) && !regions_apart(r[i], r[j])) {
+            *x = r[i].what;
+            *y = r[j].what;
+            return true;
+          }
+    }
+    lo = hi;
+  }
+  return false;
+}
+
+}  // namespace pbt

@@ -36,3 +36,18 @@ def test_rotary_dropped_while_a_call_on_another_stream_is_pending():
     assert not side.query() and table not in [t.data_ptr() for t in others]
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_clip_of_tensors_that_meet_is_refused():
+    """One tensor's result over another's gradient; norms alone may be taken of them."""
+    a, b, c = (torch.ones(2, 40, device="cuda") for _ in range(3))
+    bound = torch.ones(2, device="cuda")
+    for grads, outs in (([a, b], [c, a]), ([a, a[:, :8]], [a, b[:, :8]]), ([a[:, :20], a[:, 19:]], None)):
+        clip = binding.GradClip(grads, outs)
+        with pytest.raises(binding.PbtError, match="overlap"):
+            clip(bound)
+        assert clip().shape == (2,)
+    assert all((t == 1).all() for t in (a, b, c))
+    # the same gradient into two places is fine
+    binding.GradClip([a, a], [b, c])(bound)
+    assert torch.equal(b, c) and (b < 1).all()

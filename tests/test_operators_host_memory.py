@@ -1,0 +1,39 @@
+"""Refusals of calls whose arguments share memory: nothing here reaches a device."""
+import ctypes as C
+import os
+
+import pytest
+
+from paper_1711_09846_amd import binding
+
+EINVAL = -1
+MEM = 1 << 40      # an address that nothing reads: every call below is refused before it launches anything
+FAR = 1 << 30
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_1711_09846_amd import build
+        build.build_library(verbose=False)
+
+
+def _error():
+    return binding.lib().pbt_last_error(None).decode()
+
+
+def _clip(*tensors, P=4, max_norm=MEM + 5 * FAR, stride=1, norm=MEM + 6 * FAR, work=MEM + 7 * FAR, work_bytes=1 << 20):
+    grads = (binding.PbtGrad * len(tensors))(*[binding.PbtGrad(src, dst, n, pitch, pitch, dtype, 0) for src, dst, n, pitch, dtype in tensors])
+    return binding.lib().pbt_clip_gradients(grads, len(tensors), P, max_norm, stride, norm, work, work_bytes, None)
+
+
+@pytest.mark.parametrize("tensors", [
+    [(MEM, MEM + FAR, 100, 128, 0), (MEM + 2 * FAR, MEM, 100, 128, 0)],                     # a dst over another tensor's src
+    [(MEM, MEM + FAR, 100, 128, 0), (MEM + 2 * FAR, MEM + FAR, 100, 128, 0)],               # two tensors into one
+    [(MEM, MEM, 100, 128, 0), (MEM, MEM + FAR, 100, 128, 0)],                               # clipped in place and read by another
+    [(MEM, MEM, 100, 128, 0), (MEM + 4 * 99, MEM + 4 * 99, 29, 128, 0)],                    # columns that share an element
+    [(MEM, MEM, 100, 128, 0), (MEM + 4 * 100, MEM + 4 * 100, 29, 128, 0)],                  # the second's rows end in the first's next ones
+    [(MEM, MEM, 100, 128, 0), (MEM + 4 * 128 * 3, MEM + 4 * 128 * 3, 10, 16, 1)],           # the first's last row, another type and distance
+    [(MEM + 512 * k, MEM + 512 * k, 128, 128 * 100, 0) for k in range(100)] + [(MEM + 2 * FAR, MEM + 512 * 50 + 4, 1, 128 * 100, 0)]])
+def test_clip_tensors_that_meet_are_refused(tensors):
+    assert _clip(*tensors) == EINVAL and "overlap" in _error()
