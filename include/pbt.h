@@ -383,7 +383,8 @@ pbt_status pbt_batched_gemm_bf16(const void* d_a, int64_t lda, int64_t stride_a,
  * NULL: norms only, dst is not looked at.  d_norm (float[P], may be NULL) receives the norm before clipping.
  * Squares are summed in double, in a fixed order: no finite gradient overflows or vanishes.  A member with a NaN has norm NaN and is not
  * scaled; the factor is rounded to float; one with an infinity and no NaN has norm infinity and is multiplied by 0; a bound that is NaN does not clip, one below 0 counts as 0.
- * n_grads >= 1, 1 <= P <= PBT_MAX_P, len >= 0.  d_work: at least what pbt_clip_work_bytes says, 8-byte aligned. */
+ * n_grads >= 1, 1 <= P <= PBT_MAX_P, len >= 0.  d_work: at least what pbt_clip_work_bytes says, 8-byte aligned.
+ * d_norm, d_work, the bounds and the tensors are apart (PBT_EINVAL). */
 typedef struct {
   const void* d_src;
   void* d_dst;

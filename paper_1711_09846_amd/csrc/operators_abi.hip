@@ -3,6 +3,7 @@
 #include <cstring>
 #include <memory>
 #include <new>
+#include <utility>
 
 #include "handle.h"
 #include "operators.h"
@@ -72,26 +73,34 @@ pbt_status check_grads(const pbt_grad* g, int n, int P, bool clip) {
   return PBT_OK;
 }
 
-// What a clipping call writes is apart from everything else that it touches (a tensor's own src and dst have been looked at).
-pbt_status check_grads_apart(const pbt_grad* g, int n, int P) {
+// What a call writes is apart from everything else that it touches (a tensor's own src and dst have been looked at).  max_norm NULL: norms only, no dst is written.
+pbt_status check_grads_apart(const pbt_grad* g, int n, int P, const float* max_norm, int64_t max_norm_stride, float* norm, void* work, size_t work_bytes) {
   constexpr int FEW = 128;
   Region few[FEW];
   std::unique_ptr<Region[]> many;
   Region* r = few;
-  if (2 * (int64_t)n > FEW) {
-    many.reset(new (std::nothrow) Region[2 * (size_t)n]);
+  if (2 * (int64_t)n + 3 > FEW) {
+    many.reset(new (std::nothrow) Region[2 * (size_t)n + 3]);
     if (!(r = many.get())) return fail(nullptr, PBT_ENOMEM, "out of host memory");
   }
+  enum { NORM = -1, MAX_NORM = -2, WORK = -3 };
   int m = 0;
   for (int k = 0; k < n; ++k) {
     if (g[k].len == 0) continue;
     const int64_t e = (int64_t)elem_bytes(g[k].dtype);
-    r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_dst), g[k].len * e, g[k].dst_stride * e, P, true, k};
-    if (g[k].d_src != g[k].d_dst) r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_src), g[k].len * e, g[k].src_stride * e, P, false, k};
+    if (max_norm) r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_dst), g[k].len * e, g[k].dst_stride * e, P, true, k};
+    if (!max_norm || g[k].d_src != g[k].d_dst) r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_src), g[k].len * e, g[k].src_stride * e, P, false, k};
   }
+  if (max_norm) r[m++] = Region{reinterpret_cast<uintptr_t>(max_norm), 4, max_norm_stride * 4, max_norm_stride > 0 ? P : 1, false, MAX_NORM};
+  if (norm) r[m++] = Region{reinterpret_cast<uintptr_t>(norm), (int64_t)P * 4, 0, 1, true, NORM};
+  r[m++] = Region{reinterpret_cast<uintptr_t>(work), (int64_t)work_bytes, 0, 1, true, WORK};
   int x, y;
-  if (find_meeting(r, m, &x, &y)) return fail(nullptr, PBT_EINVAL, "dst of one of the tensors %d and %d overlaps the other", std::min(x, y), std::max(x, y));
-  return PBT_OK;
+  if (!find_meeting(r, m, &x, &y)) return PBT_OK;
+  if (x > y) std::swap(x, y);
+  if (x >= 0) return fail(nullptr, PBT_EINVAL, "dst of one of the tensors %d and %d overlaps the other", x, y);
+  const char* const names[3] = {"norm", "max_norm", "the working memory"};
+  if (y >= 0) return fail(nullptr, PBT_EINVAL, "%s overlaps tensor %d", names[-1 - x], y);
+  return fail(nullptr, PBT_EINVAL, "%s overlaps %s", names[-1 - x], names[-1 - y]);
 }
 
 // a view of heads: element (row, head, e) at base + (row row_stride + head head_stride + e)
@@ -181,7 +190,7 @@ pbt_status pbt_clip_gradients(const pbt_grad* h_grads, int32_t n_grads, int32_t 
   const size_t need = clip_work_bytes(h_grads, n_grads, P);
   if (!d_work || !aligned(d_work, 8)) return fail(nullptr, PBT_EINVAL, "work is NULL or not 8-byte aligned");
   if (work_bytes < need) return fail(nullptr, PBT_ENOMEM, "working memory: %zu bytes given, %zu needed", work_bytes, need);
-  if (d_max_norm) TRY(check_grads_apart(h_grads, n_grads, P));
+  TRY(check_grads_apart(h_grads, n_grads, P, d_max_norm, max_norm_stride, d_norm, d_work, need));
   const hipError_t e = clip_gradients(h_grads, n_grads, P, d_max_norm, max_norm_stride, d_norm, d_work, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return fail(nullptr, PBT_EDEVICE, "clipping failed to launch: %s", hipGetErrorString(e));
   return PBT_OK;

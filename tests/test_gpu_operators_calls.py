@@ -51,3 +51,17 @@ def test_clip_of_tensors_that_meet_is_refused():
     # the same gradient into two places is fine
     binding.GradClip([a, a], [b, c])(bound)
     assert torch.equal(b, c) and (b < 1).all()
+
+
+def test_clip_norms_over_the_bounds_are_refused():
+    """The bounds are read by workgroups that other members' norms do not wait for."""
+    a = torch.ones(2, 40, device="cuda")
+    bound = torch.ones(2, device="cuda")
+    with pytest.raises(binding.PbtError, match="norm"):
+        binding.GradClip([a])(bound, norms=bound)
+    both = torch.ones(2, 2, device="cuda")
+    assert binding.GradClip([a])(both[0], norms=both[1]) is not None and (both[0] == 1).all()
+    # bounds in a column beside the gradients in one array
+    store = torch.ones(3, 64, device="cuda")
+    norms = binding.GradClip([store[:, 1:64]])(store[:, 0])
+    assert torch.equal(norms, torch.full_like(norms, 63.0 ** 0.5)) and (store[:, 0] == 1).all() and (store[:, 1:] < 0.2).all()

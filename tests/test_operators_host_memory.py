@@ -37,3 +37,12 @@ def _clip(*tensors, P=4, max_norm=MEM + 5 * FAR, stride=1, norm=MEM + 6 * FAR, w
     [(MEM + 512 * k, MEM + 512 * k, 128, 128 * 100, 0) for k in range(100)] + [(MEM + 2 * FAR, MEM + 512 * 50 + 4, 1, 128 * 100, 0)]])
 def test_clip_tensors_that_meet_are_refused(tensors):
     assert _clip(*tensors) == EINVAL and "overlap" in _error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(norm=MEM + 5 * FAR), dict(norm=MEM + 5 * FAR + 12), dict(max_norm=MEM + 6 * FAR - 8, stride=1),      # norms over bounds that others still read
+    dict(norm=MEM + FAR + 4 * 127 + 4 * 128 - 8), dict(norm=MEM + 4), dict(max_norm=MEM + FAR + 400 - 4),                  # in a tensor
+    dict(max_norm=MEM + FAR + 400 - 4, stride=128), dict(work=MEM + FAR), dict(work=MEM), dict(work=MEM + 6 * FAR), dict(work=MEM + 5 * FAR),
+    dict(max_norm=None, norm=MEM + 8), dict(max_norm=None, work=MEM + 8)])
+def test_clip_norms_bounds_and_working_memory_that_meet_are_refused(kw):
+    assert _clip((MEM, MEM + FAR, 100, 128, 0), **kw) == EINVAL and "overlap" in _error()
