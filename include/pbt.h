@@ -447,7 +447,8 @@ typedef struct {                    /* device pointers, [P][d] with `stride` ele
   float *post_gain, *post_bias, *pre_gain, *pre_bias, *gate;
   int64_t stride;
 } pbt_block_params;
-/* out may lie over x, z over y (the same pitch); statistics, parameters and working memory lie apart from all matrices.  z (and its fields) is ignored with pre = NONE, gate with gate != ROWS.  d_stats: float[P * rows][4] = {mean, 1 / spread} of y and of
+/* out may lie over x, z over y (the same pitch); all else that a call writes, statistics, working memory and parameters' gradients among it, is apart from the rest
+ * of what it is given (PBT_EINVAL; matrices may be columns of the same rows).  z (and its fields) is ignored with pre = NONE, gate with gate != ROWS.  d_stats: float[P * rows][4] = {mean, 1 / spread} of y and of
  * out, for the backward pass; NULL: not kept. */
 pbt_status pbt_block_norm_forward(const pbt_block_norm* n, const pbt_rows* y, const pbt_rows* x, const pbt_rows* gate, const pbt_block_params* params,
                                   const pbt_rows* out, const pbt_rows* z, float* d_stats, void* hip_stream);

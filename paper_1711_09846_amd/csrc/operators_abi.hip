@@ -152,21 +152,41 @@ pbt_status check_params(const pbt_block_norm* n, const pbt_block_params* p, cons
   if (n->P > 1 && (q[0] || q[1] || q[2] || q[3] || q[4]) && (p->stride < n->d || p->stride > MOST)) return fail(nullptr, PBT_EINVAL, "%s: stride below d or above 2^46", what);
   return PBT_OK;
 }
-int64_t rows_bytes(const pbt_block_norm* n, const pbt_rows& m, int dtype) {
-  return n->rows == 0 ? 0 : (((int64_t)n->P * n->rows - 1) * m.pitch + n->d) * (int64_t)elem_bytes(dtype);
-}
-// an output and any other matrix of the call: apart, columns side by side in rows of one pitch, or (same_ok) the same rows
-pbt_status check_apart(const pbt_block_norm* n, const pbt_rows& out, int out_type, const char* out_name, const pbt_rows* m, int type, const char* name, bool same_ok) {
-  if (!m || !m->d || !out.d || n->rows == 0) return PBT_OK;
-  if (!overlap(out.d, rows_bytes(n, out, out_type), m->d, rows_bytes(n, *m, type))) return PBT_OK;
-  if (same_ok && out.d == m->d && out.pitch == m->pitch && out_type == type) return PBT_OK;
-  const int64_t a = (int64_t)elem_bytes(out_type), b = (int64_t)elem_bytes(type), p = out.pitch * a;
-  if (p == m->pitch * b) {
-    const int64_t diff = static_cast<const char*>(m->d) - static_cast<const char*>(out.d), at = ((diff % p) + p) % p;
-    if (at >= n->d * a && p - at >= n->d * b) return PBT_OK;
+// What a block norm's call reads and writes, by name.
+struct BlockMemory {
+  const pbt_block_norm* n;
+  Region r[24];
+  const char* names[24];
+  int count = 0;
+  void add(const void* p, int64_t bytes, int64_t stride, int64_t pieces, bool written, const char* name) {
+    if (!p) return;
+    names[count] = name;
+    r[count] = Region{reinterpret_cast<uintptr_t>(p), bytes, stride, pieces, written, count};
+    ++count;
   }
-  return fail(nullptr, PBT_EINVAL, "%s overlaps %s", out_name, name);
-}
+  void add_rows(const pbt_rows* m, int type, bool written, const char* name) {
+    if (!m || !m->d || n->rows == 0) return;
+    const int64_t e = (int64_t)elem_bytes(type), rows = n->P * n->rows;
+    if (m->pitch == n->d) add(m->d, rows * n->d * e, 0, 1, written, name);
+    else add(m->d, n->d * e, m->pitch * e, rows, written, name);
+  }
+  // an input that an output may lie over: looked at where that is not the same rows
+  void add_rows_apart_from(const pbt_rows* m, int type, const char* name, const pbt_rows& out) {
+    if (m && m->d == out.d && m->pitch == out.pitch) return;
+    add_rows(m, type, false, name);
+  }
+  void add_params(const pbt_block_params* p, bool written, const char* const* name) {
+    float* const* q = &p->post_gain;
+    for (int k = 0; k < 5; ++k) add(q[k], (int64_t)n->d * 4, p->stride * 4, n->P, written, name[k]);
+  }
+  pbt_status check() {
+    int x, y;
+    if (!find_meeting(r, count, &x, &y)) return PBT_OK;
+    return fail(nullptr, PBT_EINVAL, "%s overlaps %s", names[x], names[y]);
+  }
+};
+const char* const PARAM_NAMES[5] = {"post_gain", "post_bias", "pre_gain", "pre_bias", "the gate vector"};
+const char* const GRAD_NAMES[5] = {"the gradient of post_gain", "the gradient of post_bias", "the gradient of pre_gain", "the gradient of pre_bias", "the gate vector's gradient"};
 
 #define TRY(call) do { const pbt_status st_ = (call); if (st_ != PBT_OK) return st_; } while (0)
 
@@ -272,15 +292,19 @@ pbt_status pbt_block_norm_forward(const pbt_block_norm* n, const pbt_rows* y, co
   TRY(check_rows(n, out, "out", R, false));
   if (normed) TRY(check_rows(n, z, "z", A, false));
   if (!aligned(d_stats, 16)) return fail(nullptr, PBT_EINVAL, "stats must be 16-byte aligned");
-  TRY(check_apart(n, *out, R, "out", x, R, "x", true));
-  TRY(check_apart(n, *out, R, "out", y, A, "y", false));
-  if (gated) TRY(check_apart(n, *out, R, "out", gate, A, "the gate", false));
+  BlockMemory memory{n};
+  memory.add_rows(out, R, true, "out");
+  memory.add_rows_apart_from(x, R, "x", *out);
   if (normed) {
-    TRY(check_apart(n, *z, A, "z", y, A, "y", true));
-    TRY(check_apart(n, *z, A, "z", x, R, "x", false));
-    TRY(check_apart(n, *z, A, "z", out, R, "out", false));
-    if (gated) TRY(check_apart(n, *z, A, "z", gate, A, "the gate", false));
+    memory.add_rows(z, A, true, "z");
+    memory.add_rows_apart_from(y, A, "y", *z);
+  } else {
+    memory.add_rows(y, A, false, "y");
   }
+  if (gated) memory.add_rows(gate, A, false, "the gate");
+  memory.add(d_stats, n->P * n->rows * 16, 0, 1, true, "stats");
+  memory.add_params(params, false, PARAM_NAMES);
+  TRY(memory.check());
   BlockArgs a;
   std::memset(&a, 0, sizeof a);
   a.n = *n; a.p = *params; a.y = *y; a.x = *x; a.out = *out; a.stats = d_stats;
@@ -322,22 +346,28 @@ pbt_status pbt_block_norm_backward(const pbt_block_norm* n, const pbt_rows* y, c
     TRY(check_rows(n, dy, "dy", A, false));
     TRY(check_rows(n, dx, "dx", R, false));
     if (!d_stats || !aligned(d_stats, 16)) return fail(nullptr, PBT_EINVAL, "stats is NULL or not 16-byte aligned");
-    const struct { const pbt_rows* m; int type; const char* name; } in[5] = {{y, A, "y"}, {x, R, "x"}, {gated ? gate : nullptr, A, "the gate"},
-                                                                            {has_dz ? dz : nullptr, A, "dz"}, {has_dout ? dout : nullptr, R, "dout"}};
-    for (int k = 0; k < 5; ++k) {
-      TRY(check_apart(n, *dy, A, "dy", in[k].m, in[k].type, in[k].name, k == 3));
-      TRY(check_apart(n, *dx, R, "dx", in[k].m, in[k].type, in[k].name, k == 4));
-      if (gated) TRY(check_apart(n, *dgate, A, "dgate", in[k].m, in[k].type, in[k].name, false));
-    }
-    TRY(check_apart(n, *dy, A, "dy", dx, R, "dx", false));
-    if (gated) {
-      TRY(check_apart(n, *dgate, A, "dgate", dy, A, "dy", false));
-      TRY(check_apart(n, *dgate, A, "dgate", dx, R, "dx", false));
-    }
     const size_t need = block_norm_work_bytes(*n);
     if (!d_work || !aligned(d_work, 16)) return fail(nullptr, PBT_EINVAL, "work is NULL or not 16-byte aligned");
     if (work_bytes < need) return fail(nullptr, PBT_ENOMEM, "working memory: %zu bytes given, %zu needed", work_bytes, need);
   }
+  BlockMemory memory{n};
+  if (n->rows > 0) {
+    memory.add_rows(dy, A, true, "dy");
+    memory.add_rows(dx, R, true, "dx");
+    memory.add_rows(y, A, false, "y");
+    memory.add_rows(x, R, false, "x");
+    if (has_dz) memory.add_rows_apart_from(dz, A, "dz", *dy);
+    if (has_dout) memory.add_rows_apart_from(dout, R, "dout", *dx);
+    if (gated) {
+      memory.add_rows(dgate, A, true, "dgate");
+      memory.add_rows(gate, A, false, "the gate");
+    }
+    memory.add(d_stats, n->P * n->rows * 16, 0, 1, false, "stats");
+    memory.add(d_work, (int64_t)block_norm_work_bytes(*n), 0, 1, true, "the working memory");
+  }
+  memory.add_params(params, false, PARAM_NAMES);
+  memory.add_params(grads, true, GRAD_NAMES);
+  TRY(memory.check());
   BlockArgs a;
   std::memset(&a, 0, sizeof a);
   a.n = *n; a.p = *params; a.g = *grads;

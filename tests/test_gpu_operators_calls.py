@@ -65,3 +65,24 @@ def test_clip_norms_over_the_bounds_are_refused():
     store = torch.ones(3, 64, device="cuda")
     norms = binding.GradClip([store[:, 1:64]])(store[:, 0])
     assert torch.equal(norms, torch.full_like(norms, 63.0 ** 0.5)) and (store[:, 0] == 1).all() and (store[:, 1:] < 0.2).all()
+
+
+def test_block_norm_gradients_into_one_tensor_are_refused():
+    """Two parameters' gradients into the same memory, or over a parameter; columns of one store are fine."""
+    P, rows, d = 2, 6, 40
+    g = _gen(2)
+    y, x, dout, dz = (_normal(g, P * rows, d) for _ in range(4))
+    params = dict(post_gain=1 + _normal(g, P, d, scale=0.1), pre_gain=1 + _normal(g, P, d, scale=0.1))
+    op = binding.BlockNorm(d, members=P)
+    _, _, stats = op.forward(y, x, params)
+    _, _, _, want = op.backward(y, x, params, stats, dout, dz)
+    one = torch.zeros(P, d, device="cuda")
+    for grads in (dict(post_gain=one, pre_gain=one), dict(post_gain=one, pre_gain=params["pre_gain"])):
+        with pytest.raises(binding.PbtError, match="overlaps"):
+            op.backward(y, x, params, stats, dout, dz, grads=grads)
+    store = torch.zeros(P, 100, device="cuda")
+    grads = dict(post_gain=store[:, 1:41], pre_gain=store[:, 41:81])
+    op.backward(y, x, params, stats, dout, dz, grads=grads)
+    assert all(torch.equal(grads[k], want[k]) for k in want) and not store[:, 0].any() and not store[:, 81:].any()
+    with pytest.raises(binding.PbtError, match="overlaps"):
+        op.forward(y, x, params, out=x, z=x)

@@ -46,3 +46,57 @@ def test_clip_tensors_that_meet_are_refused(tensors):
     dict(max_norm=None, norm=MEM + 8), dict(max_norm=None, work=MEM + 8)])
 def test_clip_norms_bounds_and_working_memory_that_meet_are_refused(kw):
     assert _clip((MEM, MEM + FAR, 100, 128, 0), **kw) == EINVAL and "overlap" in _error()
+
+
+def _at(k, pitch=64):
+    return binding.PbtRows(MEM + (k << 24), pitch)
+
+
+def _place(k):
+    return MEM + ((16 + k) << 24)
+
+
+def _settings(**kw):
+    k = dict(rows=10, P=2, d=64, post=1, pre=2, gate=0, gate_act=0, dtype=1, res_dtype=0, eps=1e-5, alpha=1.0, beta=1.0)
+    k.update(kw)
+    return binding.PbtBlockNorm(**k)
+
+
+def _forward(n, stats=_place(0), params=None, **kw):
+    a = dict(y=_at(0), x=_at(1), gate=_at(2), out=_at(3), z=_at(4))
+    a.update(kw)
+    return binding.lib().pbt_block_norm_forward(C.byref(n), *[C.byref(a[k]) for k in ("y", "x", "gate")], C.byref(params or binding.PbtBlockParams(stride=64)), C.byref(a["out"]),
+                                                C.byref(a["z"]), stats, None)
+
+
+def _backward(n, stats=_place(0), params=None, grads=None, work=_place(1), **kw):
+    a = dict(y=_at(0), x=_at(1), gate=_at(2), dout=_at(3), dz=_at(4), dy=_at(5), dx=_at(6), dgate=_at(7))
+    a.update(kw)
+    none = binding.PbtBlockParams(stride=64)
+    return binding.lib().pbt_block_norm_backward(C.byref(n), *[C.byref(a[k]) for k in ("y", "x", "gate")], C.byref(params or none), stats,
+                                                 *[C.byref(a[k]) for k in ("dout", "dz", "dy", "dx", "dgate")], C.byref(grads or none), work, 1 << 24, None)
+
+
+def _params(stride=64, **kw):
+    return binding.PbtBlockParams(stride=stride, **kw)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(stats=_at(0).d), dict(stats=_at(3).d + 16), dict(stats=_at(4).d), dict(params=_params(post_gain=_place(0) + 64)),     # statistics over matrices and a parameter
+    dict(params=_params(pre_bias=_at(3).d + 64)), dict(params=_params(pre_gain=_at(4).d)),                                       # outputs over parameters
+    dict(n=_settings(gate=1), params=_params(gate=_at(4).d + 64, stride=128))])
+def test_block_norm_forward_statistics_and_parameters_that_meet_outputs_are_refused(kw):
+    kw = dict(kw)
+    assert _forward(kw.pop("n", _settings()), **kw) == EINVAL and "overlap" in _error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(grads=_params(post_gain=_place(2), pre_gain=_place(2))), dict(grads=_params(post_gain=_place(2), pre_bias=_place(2) + 252)),
+    dict(grads=_params(post_gain=_place(2), post_bias=_place(2) + 4 * 96, stride=128)),                      # rows that run into the next member's
+    dict(params=_params(pre_gain=_place(2)), grads=_params(pre_gain=_place(2))),                             # over the parameter
+    dict(grads=_params(pre_gain=_at(4).d)), dict(grads=_params(pre_gain=_at(6).d)), dict(grads=_params(pre_gain=_place(0))), dict(grads=_params(pre_gain=_place(1))),
+    dict(work=_at(0).d), dict(work=_at(6).d), dict(work=_place(0)), dict(stats=_at(5).d), dict(params=_params(pre_gain=_at(5).d)),
+    dict(n=_settings(rows=0), grads=_params(post_gain=_place(2), pre_gain=_place(2)))])
+def test_block_norm_backward_gradients_and_working_memory_that_meet_are_refused(kw):
+    kw = dict(kw)
+    assert _backward(kw.pop("n", _settings()), **kw) == EINVAL and "overlap" in _error()
