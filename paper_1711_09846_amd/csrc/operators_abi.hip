@@ -103,18 +103,12 @@ pbt_status check_grads_apart(const pbt_grad* g, int n, int P, const float* max_n
   return fail(nullptr, PBT_EINVAL, "%s overlaps %s", names[-1 - x], names[-1 - y]);
 }
 
-// a view of heads: element (row, head, e) at base + (row row_stride + head head_stride + e)
-struct HeadView { const void* base; int64_t row, head, heads; };
-// no element of `a` is one of `b`: their memory is apart, or they are columns of the same rows
-bool heads_apart(const HeadView& a, const HeadView& b, int64_t rows, int width, int64_t e) {
-  const int64_t a_row = ((a.heads - 1) * a.head + width) * e, b_row = ((b.heads - 1) * b.head + width) * e;   // bytes of a row's heads
-  if (!overlap(a.base, (rows - 1) * a.row * e + a_row, b.base, (rows - 1) * b.row * e + b_row)) return true;
-  if (rows == 1 || a.row != b.row || a.row <= 0) return false;
-  const int64_t p = a.row * e, diff = static_cast<const char*>(b.base) - static_cast<const char*>(a.base), m = ((diff % p) + p) % p;
-  return m >= a_row && p - m >= b_row;
+HeadView src_view(const pbt_heads& g, int64_t rows, int width, int64_t e) {
+  return HeadView{reinterpret_cast<uintptr_t>(g.d_src), g.src_row * e, g.src_head * e, rows, g.heads, width * e};
 }
-HeadView src_view(const pbt_heads& g) { return HeadView{g.d_src, g.src_row, g.src_head, g.heads}; }
-HeadView dst_view(const pbt_heads& g) { return HeadView{g.d_dst, g.dst_row, g.dst_head, g.heads}; }
+HeadView dst_view(const pbt_heads& g, int64_t rows, int width, int64_t e) {
+  return HeadView{reinterpret_cast<uintptr_t>(g.d_dst), g.dst_row * e, g.dst_head * e, rows, g.heads, width * e};
+}
 bool same_view(const pbt_heads& g, int64_t rows) {
   return g.d_src == g.d_dst && (rows == 1 || g.src_row == g.dst_row) && (g.heads == 1 || g.src_head == g.dst_head);
 }
@@ -256,12 +250,15 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
     // dst's elements are apart: heads within rows, or rows within heads
     const bool in_rows = g.dst_row >= (g.heads - 1) * g.dst_head + width, in_heads = g.dst_row >= width && g.dst_head >= (rows - 1) * g.dst_row + width;
     if (rows > 1 && !(g.heads == 1 ? g.dst_row >= width : in_rows || in_heads)) return fail(nullptr, PBT_EINVAL, "group %d: rows of dst overlap", k);
-    if (!same_view(g, rows) && !heads_apart(src_view(g), dst_view(g), rows, width, e)) return fail(nullptr, PBT_EINVAL, "group %d: dst overlaps src and is not the same view", k);
+    if (!same_view(g, rows) && !heads_apart(src_view(g, rows, width, e), dst_view(g, rows, width, e))) return fail(nullptr, PBT_EINVAL, "group %d: dst overlaps src and is not the same view", k);
   }
   for (int k = 0; k < n_groups && rows > 0; ++k)
-    for (int j = 0; j < n_groups; ++j)
-      if (j != k && !(heads_apart(dst_view(h_groups[k]), src_view(h_groups[j]), rows, width, e) && heads_apart(dst_view(h_groups[k]), dst_view(h_groups[j]), rows, width, e)))
+    for (int j = 0; j < n_groups; ++j) {
+      if (j == k) continue;
+      const HeadView out = dst_view(h_groups[k], rows, width, e);
+      if (!heads_apart(out, src_view(h_groups[j], rows, width, e)) || !heads_apart(out, dst_view(h_groups[j], rows, width, e)))
         return fail(nullptr, PBT_EINVAL, "dst of group %d overlaps group %d", k, j);
+    }
   if (heads > 32768) return fail(nullptr, PBT_EINVAL, "more than 32768 heads");
   if (rows == 0) return PBT_OK;
   RotaryArgs a;

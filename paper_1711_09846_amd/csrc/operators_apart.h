@@ -86,4 +86,33 @@ inline bool find_meeting(Region* r, int n, int* x, int* y) {
   return false;
 }
 
+// Heads of `width` bytes at at + i row + j head.
+struct HeadView { uintptr_t at; int64_t row, head, rows, heads, width; };
+
+// No byte of `a` is one of `b`; false too where strides are too different to tell.
+inline bool heads_apart(HeadView a, HeadView b) {
+  const auto span = [](const HeadView& v) { return (v.rows - 1) * v.row + (v.heads - 1) * v.head + v.width; };
+  if (a.at >= b.at + (uintptr_t)span(b) || b.at >= a.at + (uintptr_t)span(a)) return true;
+  if (a.rows == 1 && b.rows == 1) {
+    a.row = a.head * a.heads + a.width;
+    b.row = b.head * b.heads + b.width;
+    a.row = b.row = std::max(a.row, b.row) * 2;
+  }
+  // the longer of both strides is the same, and what the shorter one spans lies within it: places within one such frame, and in the next one
+  const auto frames = [](const HeadView& x, const HeadView& y) {
+    if (x.row != y.row || x.row <= 0) return false;
+    const Region rx{0, x.width, x.head, x.heads, true, 0};
+    if (region_span(rx) > x.row || (y.heads - 1) * y.head + y.width > y.row) return false;
+    const int64_t p = x.row, d = (int64_t)(y.at - x.at), m = ((d % p) + p) % p;
+    // (addresses within the frame, moved up by one frame so that none is negative)
+    const Region x1{(uintptr_t)p, x.width, x.head, x.heads, true, 0};
+    const Region y1{(uintptr_t)(p + m), y.width, y.head, y.heads, true, 0}, y0{(uintptr_t)m, y.width, y.head, y.heads, true, 0};
+    return regions_apart(x1, y1) && regions_apart(x1, y0);
+  };
+  if (frames(a, b)) return true;
+  // heads outermost
+  const auto turned = [](const HeadView& v, int64_t head) { return HeadView{v.at, v.heads > 1 ? v.head : head, v.row, v.heads, v.rows, v.width}; };
+  return (a.heads > 1 || b.heads > 1) && frames(turned(a, b.head), turned(b, a.head));
+}
+
 }  // namespace pbt

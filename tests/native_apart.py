@@ -16,6 +16,11 @@ extern "C" int meeting(const long long* fields, int n, int* out) {
   delete[] r;
   return found;
 }
+// fields: address, row, head, rows, heads, width of both
+extern "C" int heads_apart(const long long* f) {
+  const auto view = [](const long long* v) { return pbt::HeadView{(uintptr_t)v[0], v[1], v[2], v[3], v[4], v[5]}; };
+  return pbt::heads_apart(view(f), view(f + 6));
+}
 """
 
 
@@ -34,3 +39,8 @@ def meeting(regions):
     flat = [int(v) for r in regions for v in r]
     out = (ctypes.c_int * 2)()
     return tuple(out) if _lib().meeting((ctypes.c_longlong * len(flat))(*flat), len(regions), out) else None
+
+
+def heads_apart(a, b):
+    """a, b: (address, row, head, rows, heads, width) in bytes."""
+    return bool(_lib().heads_apart((ctypes.c_longlong * 12)(*a, *b)))

@@ -86,3 +86,32 @@ def test_block_norm_gradients_into_one_tensor_are_refused():
     assert all(torch.equal(grads[k], want[k]) for k in want) and not store[:, 0].any() and not store[:, 81:].any()
     with pytest.raises(binding.PbtError, match="overlaps"):
         op.forward(y, x, params, out=x, z=x)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("order", ["head-part", "row-outermost-padded", "heads-outermost"])
+def test_rotary_of_query_and_key_heads_that_lie_side_by_side(dtype, order):
+    """A joint projection with a head's query, key and value next to one another: both turned in place in one call, values as they were."""
+    rows, heads, w = 33, 5, 24
+    g = _gen(4)
+    if order == "heads-outermost":
+        joint = _normal(g, heads, rows, 3, w, dtype=dtype).transpose(0, 1)
+    elif order == "head-part":
+        joint = _normal(g, rows, heads, 3, w, dtype=dtype)
+    else:
+        joint = _normal(g, rows, heads * 3 * w + 7, dtype=dtype)[:, 3:3 + heads * 3 * w].unflatten(1, (heads, 3, w))
+    keep = joint.clone()
+    r = binding.Rotary(18)
+    q, k = joint[:, :, 0], joint[:, :, 1]
+    want = [r(t, torch.empty(rows, heads, w, dtype=dtype, device="cuda"), start=3) for t in (q, k)]
+    r([q, k], start=3)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(joint[:, :, 2], keep[:, :, 2])
+    # from queries into the place of the values
+    back = r(q, torch.empty(rows, heads, w, dtype=dtype, device="cuda"), start=3, backward=True)
+    r(q, joint[:, :, 2], start=3, backward=True)
+    assert torch.equal(q, want[0]) and torch.equal(joint[:, :, 2], back) and torch.equal(k, want[1])
+    # half of a query and half of a key
+    if order == "head-part":
+        flat = joint.flatten(1)
+        with pytest.raises(binding.PbtError, match="overlaps"):
+            r([q, flat[:, w // 2:w // 2 + heads * 3 * w - 2 * w].unfold(1, w, 3 * w)], start=3)
