@@ -409,7 +409,9 @@ pbt_status pbt_clip_gradients(const pbt_grad* h_grads, int32_t n_grads, int32_t 
 /* Writes the table of frequencies, rot_dim / 2 doubles (in turns per position), that pbt_rotary_apply reads; d_table is 8-byte aligned. */
 pbt_status pbt_rotary_plan(const pbt_rotary* r, void* d_table, size_t table_bytes, void* hip_stream);
 /* One group of heads: element (row, head, e) at d_src[row * src_row + head * src_head + e].  dst is src with the same strides (in
- * place), or the two share no element; nor do a dst and another group (at most 32768 heads in all, of at most 16384 elements). */
+ * place), or the two share no element; nor do a dst and another group (at most 32768 heads in all, of at most 16384 elements).  Heads of a row are at least
+ * `width` apart, strides are 0..2^31, rows span at most 2^46 elements.  Whether memory is shared is told where rows (or, with heads outermost, heads) are
+ * equally far apart on both sides; other views count as meeting where their spans do (PBT_EINVAL). */
 typedef struct {
   const void* d_src;
   void* d_dst;

@@ -247,6 +247,7 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
     const int64_t limit = (int64_t)1 << 31;
     if (g.src_row < 0 || g.dst_row < 0 || g.src_head > limit || g.dst_head > limit || g.src_row > limit || g.dst_row > limit)
       return fail(nullptr, PBT_EINVAL, "group %d: strides above 2^31 or negative", k);
+    if (rows > 1 && std::max(g.src_row, g.dst_row) > MOST / (rows - 1)) return fail(nullptr, PBT_EINVAL, "group %d: rows span more than 2^46 elements", k);
     // dst's elements are apart: heads within rows, or rows within heads
     const bool in_rows = g.dst_row >= (g.heads - 1) * g.dst_head + width, in_heads = g.dst_row >= width && g.dst_head >= (rows - 1) * g.dst_row + width;
     if (rows > 1 && !(g.heads == 1 ? g.dst_row >= width : in_rows || in_heads)) return fail(nullptr, PBT_EINVAL, "group %d: rows of dst overlap", k);

@@ -100,3 +100,16 @@ def test_block_norm_forward_statistics_and_parameters_that_meet_outputs_are_refu
 def test_block_norm_backward_gradients_and_working_memory_that_meet_are_refused(kw):
     kw = dict(kw)
     assert _backward(kw.pop("n", _settings()), **kw) == EINVAL and "overlap" in _error()
+
+
+def _rotary(rows, dtype=0, **kw):
+    g = dict(d_src=MEM, d_dst=MEM, src_row=64, src_head=64, dst_row=64, dst_head=64, heads=1, unused=0)
+    g.update(kw)
+    s = binding.PbtRotary(64, 0, 0, 0, 10000.0, 1.0, 0.0, 1.0, 32.0, 1.0)
+    return binding.lib().pbt_rotary_apply(C.byref(s), MEM + FAR, (binding.PbtHeads * 1)(binding.PbtHeads(**g)), 1, dtype, rows, 64, None, 0, 0, 0, 0, None)
+
+
+@pytest.mark.parametrize("kw", [dict(src_row=1 << 31, dst_row=64, d_dst=MEM + (1 << 50)), dict(src_row=1 << 31, dst_row=1 << 31), dict(src_row=64, dst_row=1 << 31, d_dst=MEM + 4)])
+def test_rotary_rows_that_span_more_than_addresses_are_refused(kw):
+    """2^31 rows, 2^31 elements of 4 bytes apart: 2^64 bytes."""
+    assert _rotary((1 << 31) - 1, **kw) == EINVAL and "2^46" in _error()
