@@ -422,7 +422,7 @@ typedef struct {
 /* Turns h_groups[0 .. n_groups) (1 to 4: query and key heads of one call share their angles) of `rows` rows and `width` elements a
  * head.  Position of row r: d_positions[r] (int32 or int64 by position_bytes 4 or 8), or with d_positions = NULL
  * start + (period > 0 ? r % period : r).  backward = 1 applies the transposed rotation (the same gain, the angle
- * negated): the gradient of the input from that of the output.  rows = 0 is allowed. */
+ * negated): the gradient of the input from that of the output.  rows = 0 is allowed.  Positions and table are apart from every dst (PBT_EINVAL). */
 pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_heads* h_groups, int32_t n_groups, int32_t dtype, int64_t rows,
                             int32_t width, const void* d_positions, int32_t position_bytes, int64_t start, int64_t period, int32_t backward,
                             void* hip_stream);

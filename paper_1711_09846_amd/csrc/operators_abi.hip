@@ -260,6 +260,12 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
       if (!heads_apart(out, src_view(h_groups[j], rows, width, e)) || !heads_apart(out, dst_view(h_groups[j], rows, width, e)))
         return fail(nullptr, PBT_EINVAL, "dst of group %d overlaps group %d", k, j);
     }
+  for (int k = 0; k < n_groups && rows > 0; ++k) {
+    const HeadView out = dst_view(h_groups[k], rows, width, e);
+    const auto under = [&](const void* p, int64_t bytes) { return p && !heads_apart(out, HeadView{reinterpret_cast<uintptr_t>(p), out.row, 0, 1, 1, bytes}); };
+    if (under(d_positions, rows * position_bytes)) return fail(nullptr, PBT_EINVAL, "dst of group %d overlaps the positions", k);
+    if (under(d_table, r->rot_dim / 2 * 8)) return fail(nullptr, PBT_EINVAL, "dst of group %d overlaps the table", k);
+  }
   if (heads > 32768) return fail(nullptr, PBT_EINVAL, "more than 32768 heads");
   if (rows == 0) return PBT_OK;
   RotaryArgs a;

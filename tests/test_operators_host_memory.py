@@ -113,3 +113,14 @@ def _rotary(rows, dtype=0, **kw):
 def test_rotary_rows_that_span_more_than_addresses_are_refused(kw):
     """2^31 rows, 2^31 elements of 4 bytes apart: 2^64 bytes."""
     assert _rotary((1 << 31) - 1, **kw) == EINVAL and "2^46" in _error()
+
+
+def _rotary_reads(positions, table=MEM + FAR, dst_row=64, rows=100):
+    heads = (binding.PbtHeads * 1)(binding.PbtHeads(MEM, MEM, dst_row, 64, dst_row, 64, 1, 0))
+    s = binding.PbtRotary(64, 0, 0, 0, 10000.0, 1.0, 0.0, 1.0, 32.0, 1.0)
+    return binding.lib().pbt_rotary_apply(C.byref(s), table, heads, 1, 0, rows, 64, positions, 4, 0, 0, 0, None)
+
+
+@pytest.mark.parametrize("kw", [dict(positions=MEM), dict(positions=MEM + 100 * 256 - 4), dict(positions=MEM - 4), dict(positions=MEM + 256, dst_row=128), dict(positions=None, table=MEM + 512)])
+def test_rotary_positions_and_table_under_the_heads_are_refused(kw):
+    assert _rotary_reads(**kw) == EINVAL and "overlap" in _error()
