@@ -453,6 +453,13 @@ def _call(device, fn, *args):
         raise PbtError(rc, lib().pbt_last_error(None).decode())
 
 
+def _no_graph(tensors):
+    """Results have no graph: where one would be recorded, losing it is refused."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise ValueError("the results would have no graph, and a tensor of the call requires a gradient: call under torch.no_grad(), or from an autograd.Function")
+
+
 def _dtype_code(t):
     import torch
     if t.dtype == torch.bfloat16:
@@ -485,7 +492,8 @@ class GradClip:
     and types), None: clipped in place.  The tensors are kept, as an optimiser keeps its parameters.  A tensor may be listed once only, and where
     one's clipped gradient goes is no part of another.
     Calling it computes the norms [P] (float32) and, with max_norm (float32 tensor [P], any stride, or of one element for all members),
-    scales every member whose norm is larger.  Without max_norm only the norms are computed."""
+    scales every member whose norm is larger.  Without max_norm only the norms are computed.  As in an optimiser, no graph is recorded through
+    either, whether or not the tensors require a gradient."""
 
     def __init__(self, grads, outs=None):
         grads = list(grads)
@@ -553,7 +561,8 @@ class Rotary:
     def __call__(self, src, dst=None, positions=None, start=0, period=0, backward=False):
         """src: tensor [rows, heads, width] with adjacent elements, or up to four of them (query and key heads); dst: the same, None: in place.
         positions: int32 or int64 tensor [rows]; without them row r is at start + (r % period if period else r).  backward: the transposed
-        rotation, for gradients.  Returns dst."""
+        rotation, for gradients.  Returns dst, which has no graph: a call on tensors that require a gradient is refused unless gradients are off
+        (torch.no_grad(), the inside of an autograd.Function)."""
         import torch
         if dst is None:
             dst = src
@@ -561,6 +570,9 @@ class Rotary:
         srcs, dsts = (src, dst) if many else ((src,), (dst,))
         if not srcs or len(srcs) != len(dsts):
             raise ValueError("as many dst as src are wanted, and at least one")
+        if torch.is_grad_enabled():
+            _no_graph(srcs)
+            _no_graph(dsts)
         first = srcs[0]
         groups = (PbtHeads * len(srcs))()
         for g, a, b in zip(groups, srcs, dsts):
@@ -664,8 +676,13 @@ class BlockNorm:
         return out
 
     def forward(self, y, x, params=None, gate=None, out=None, z=None, stats=True):
-        """Returns (out, z, stats); z is None with pre = "none", stats (float32 [rows, 4], for backward) with stats = False."""
+        """Returns (out, z, stats); z is None with pre = "none", stats (float32 [rows, 4], for backward) with stats = False.  They have no graph
+        (`backward` has the gradients): a call on tensors that require one is refused unless gradients are off (torch.no_grad(), the inside of an autograd.Function)."""
         import torch
+        if torch.is_grad_enabled():
+            _no_graph((y, x, gate, out, z))
+            if params:
+                _no_graph(params.values())
         s, _ = self._settings(y, x)
         device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
         if device.type != "cuda":

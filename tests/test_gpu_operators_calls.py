@@ -115,3 +115,42 @@ def test_rotary_of_query_and_key_heads_that_lie_side_by_side(dtype, order):
         flat = joint.flatten(1)
         with pytest.raises(binding.PbtError, match="overlaps"):
             r([q, flat[:, w // 2:w // 2 + heads * 3 * w - 2 * w].unfold(1, w, 3 * w)], start=3)
+
+
+def test_calls_that_would_lose_a_graph_are_refused():
+    """Under gradient mode a tensor that requires a gradient is refused; without it, and inside an autograd.Function, it is not."""
+    x = torch.randn(6, 2, 8, generator=_gen(5)).cuda()
+    leaf = x.clone().requires_grad_()
+    r = binding.Rotary(8)
+    empty = lambda: torch.empty(6, 2, 8, device="cuda")  # noqa: E731
+    for src, dst in ((leaf, empty()), ([x, leaf], [empty(), empty()]), (x, leaf), (leaf * 2, empty())):
+        with pytest.raises(ValueError, match="graph"):
+            r(src, dst)
+
+    class Turn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, t):
+            return r(t, torch.empty_like(t), start=3)
+
+        @staticmethod
+        def backward(ctx, g):
+            return r(g.contiguous(), torch.empty_like(g), start=3, backward=True)
+
+    w = torch.randn(6, 2, 8, generator=_gen(6)).cuda()
+    (Turn.apply(leaf) * w).sum().backward()
+    with torch.no_grad():
+        assert torch.equal(leaf.grad, r(w, torch.empty_like(w), start=3, backward=True))
+        r(leaf, empty())
+
+    y, h, gain = torch.randn(6, 16, generator=_gen(7)).cuda(), torch.randn(6, 16, generator=_gen(8)).cuda(), torch.ones(16, device="cuda")
+    op = binding.BlockNorm(16)
+    want = op.forward(y, h, dict(pre_gain=gain))
+    for args in ((y.clone().requires_grad_(), h, {}), (y, h.clone().requires_grad_(), {}), (y, h, dict(pre_gain=gain.clone().requires_grad_()))):
+        with pytest.raises(ValueError, match="graph"):
+            op.forward(*args)
+        with torch.no_grad():
+            op.forward(*args)
+    # gradients are what backward hands out itself
+    param = dict(pre_gain=gain.clone().requires_grad_())
+    grads = op.backward(y, h, param, want[2], h, y)[3]
+    assert grads["pre_gain"].shape == (1, 16) and not grads["pre_gain"].requires_grad
