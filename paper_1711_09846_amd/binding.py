@@ -434,23 +434,29 @@ BLOCK_PARAMS = ("post_gain", "post_bias", "pre_gain", "pre_bias", "gate")
 
 
 @functools.lru_cache(None)
-def _stream_of():
-    """Device index -> handle of its current stream, without the Python object around it where torch offers that (2 of the 9 us of a small call)."""
+def _runtime():
+    """(the current device's index, device index -> handle of its current stream, marks tensors as written for autograd's version check): functions, without
+    the Python around them where torch offers that (a small call takes 8 us in all)."""
     import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    index = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return index, stream, getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
 
 
-def _call(device, fn, *args):
-    """fn(*args, stream) with the device's current stream; kernels are launched on the current device, so it is made current if it is not."""
-    import torch
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, _stream_of()(device.index))
+def _call(device, fn, *args, written=()):
+    """fn(*args, stream) with the device's current stream; kernels are launched on the current device, so it is made current if it is not.  written: tensors
+    of the caller that the call writes."""
+    current, stream_of, mark = _runtime()
+    if current() == device.index:
+        rc = fn(*args, stream_of(device.index))
     else:
+        import torch
         with torch.cuda.device(device):
-            rc = fn(*args, _stream_of()(device.index))
+            rc = fn(*args, stream_of(device.index))
     if rc != 0:
         raise PbtError(rc, lib().pbt_last_error(None).decode())
+    if written:
+        mark(written)
 
 
 def _no_graph(tensors):
@@ -460,13 +466,17 @@ def _no_graph(tensors):
             raise ValueError("the results would have no graph, and a tensor of the call requires a gradient: call under torch.no_grad(), or from an autograd.Function")
 
 
-def _dtype_code(t):
+@functools.lru_cache(None)
+def _dtype_codes():
     import torch
-    if t.dtype == torch.bfloat16:
-        return 1
-    if t.dtype == torch.float32:
-        return 0
-    raise ValueError("float32 or bfloat16 tensors are wanted, not %s" % t.dtype)
+    return {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _dtype_code(t):
+    code = _dtype_codes().get(t.dtype)
+    if code is None:
+        raise ValueError("float32 or bfloat16 tensors are wanted, not %s" % t.dtype)
+    return code
 
 
 def _choice(table, value, what):
@@ -496,6 +506,8 @@ class GradClip:
     either, whether or not the tensors require a gradient."""
 
     def __init__(self, grads, outs=None):
+        import torch
+        self.torch = torch
         grads = list(grads)
         outs = grads if outs is None else list(outs)
         if not grads or len(outs) != len(grads):
@@ -514,6 +526,8 @@ class GradClip:
         if len({e.d_dst for e in table if e.len}) < sum(1 for e in table if e.len):
             raise ValueError("a tensor is listed twice")
         self.grads, self.outs, self._table = grads, outs, table
+        # (views of one tensor share the count of its versions)
+        self._written = tuple({id(b): b for b in (t if t._base is None else t._base for t in outs)}.values())
         n = C.c_size_t()
         rc = lib().pbt_clip_work_bytes(table, len(grads), self.P, C.byref(n))
         if rc != 0:
@@ -521,18 +535,22 @@ class GradClip:
         self._work_bytes = n.value
 
     def __call__(self, max_norm=None, norms=None):
-        import torch
+        torch = self.torch
+        written = () if max_norm is None else self._written
         if norms is None:
             norms = torch.empty(self.P, dtype=torch.float32, device=self.device)
         elif norms.shape != (self.P,) or norms.dtype != torch.float32 or not norms.is_contiguous() or norms.device != self.device:
             raise ValueError("norms: a contiguous float32 tensor [P] on the gradients' device")
+        else:
+            written = (*written, norms)
         ptr = stride = 0
         if max_norm is not None:
             if max_norm.dtype != torch.float32 or max_norm.device != self.device or (max_norm.numel() != 1 and max_norm.shape != (self.P,)):
                 raise ValueError("max_norm: a float32 tensor [P], or of one element, on the gradients' device")
             ptr, stride = max_norm.data_ptr(), 0 if max_norm.numel() == 1 else max_norm.stride(0)
         work = torch.empty(self._work_bytes, dtype=torch.uint8, device=self.device)   # (of this call: calls on two streams do not meet in it)
-        _call(self.device, lib().pbt_clip_gradients, self._table, len(self.grads), self.P, ptr, stride, norms.data_ptr(), work.data_ptr(), self._work_bytes)
+        _call(self.device, lib().pbt_clip_gradients, self._table, len(self.grads), self.P, ptr, stride, norms.data_ptr(), work.data_ptr(), self._work_bytes,
+              written=written)
         return norms
 
 
@@ -548,6 +566,7 @@ class Rotary:
 
     def __init__(self, rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained=0.0, low=1.0, high=32.0, gain=1.0, device="cuda:0"):
         import torch
+        self.torch = torch
         self.settings = rotary_settings(rot_dim, base, layout, scaling, factor, trained, low, high, gain)
         self.device = torch.device(device)
         if self.device.index is None:
@@ -563,7 +582,7 @@ class Rotary:
         positions: int32 or int64 tensor [rows]; without them row r is at start + (r % period if period else r).  backward: the transposed
         rotation, for gradients.  Returns dst, which has no graph: a call on tensors that require a gradient is refused unless gradients are off
         (torch.no_grad(), the inside of an autograd.Function)."""
-        import torch
+        torch = self.torch
         if dst is None:
             dst = src
         many = isinstance(src, (list, tuple))
@@ -571,8 +590,7 @@ class Rotary:
         if not srcs or len(srcs) != len(dsts):
             raise ValueError("as many dst as src are wanted, and at least one")
         if torch.is_grad_enabled():
-            _no_graph(srcs)
-            _no_graph(dsts)
+            _no_graph((*srcs, *dsts))
         first = srcs[0]
         groups = (PbtHeads * len(srcs))()
         for g, a, b in zip(groups, srcs, dsts):
@@ -590,10 +608,10 @@ class Rotary:
             if positions.shape != (first.shape[0],) or positions.dtype not in (torch.int32, torch.int64) or not positions.is_contiguous() or positions.device != self.device:
                 raise ValueError("positions: a contiguous int32 or int64 tensor [rows] on the table's device")
             pos, size = positions.data_ptr(), positions.element_size()
-        if _stream_of()(self.device.index) != self._stream:
+        if _runtime()[1](self.device.index) != self._stream:
             self.table.record_stream(torch.cuda.current_stream(self.device))   # (the table's memory is that stream's: not given away before this one is done)
         _call(self.device, lib().pbt_rotary_apply, C.byref(self.settings), self.table.data_ptr(), groups, len(srcs), _dtype_code(first), first.shape[0], first.shape[2],
-              pos, size, start, period, int(bool(backward)))
+              pos, size, start, period, int(bool(backward)), written=dsts)
         return dst
 
 
@@ -604,6 +622,8 @@ class BlockNorm:
     with the same distance between members."""
 
     def __init__(self, width, members=1, post="layer", pre="layer", gate="none", act="none", eps=1e-5, alpha=1.0, beta=1.0):
+        import torch
+        self.torch = torch
         self.width, self.members = width, members
         self.settings = PbtBlockNorm(0, members, width, _choice(_NORMS, post, "post"), _choice(_NORMS, pre, "pre"), _choice(_GATES, gate, "gate"),
                                      _choice(_GATE_ACTS, act, "act"), 0, 0, eps, alpha, beta)
@@ -649,7 +669,7 @@ class BlockNorm:
 
     def _params(self, params, device):
         """The fields of pbt_block_params."""
-        import torch
+        torch = self.torch
         if not params:
             return 0, 0, 0, 0, 0, self.width
         out, stride, seen = [], None, 0
@@ -678,17 +698,16 @@ class BlockNorm:
     def forward(self, y, x, params=None, gate=None, out=None, z=None, stats=True):
         """Returns (out, z, stats); z is None with pre = "none", stats (float32 [rows, 4], for backward) with stats = False.  They have no graph
         (`backward` has the gradients): a call on tensors that require one is refused unless gradients are off (torch.no_grad(), the inside of an autograd.Function)."""
-        import torch
+        torch = self.torch
         if torch.is_grad_enabled():
-            _no_graph((y, x, gate, out, z))
-            if params:
-                _no_graph(params.values())
+            _no_graph((y, x, gate, out, z, *params.values()) if params else (y, x, gate, out, z))
         s, _ = self._settings(y, x)
         device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
         if device.type != "cuda":
             raise ValueError("device tensors are wanted")
         if gate is not None and not self._rows_gate:
             raise ValueError("a gate's matrix goes with gate = \"rows\"")
+        written = [t for t in (out, z) if t is not None]
         if out is None:
             out = torch.empty_like(x)
         if not self._pre:
@@ -700,19 +719,20 @@ class BlockNorm:
         a = _I64x16(*rows(y, shape, ty, device, "y"), *rows(x, shape, tx, device, "x"), *rows(gate, shape, ty, device, "gate"),
                     *rows(out, shape, tx, device, "out"), *rows(z, shape, ty, device, "z"), *self._params(params, device))
         at = C.addressof(a)
-        _call(device, lib().pbt_block_norm_forward, C.byref(s), at, at + 16, at + 32, at + 80, at + 48, at + 64, 0 if st is None else st.data_ptr())
+        _call(device, lib().pbt_block_norm_forward, C.byref(s), at, at + 16, at + 32, at + 80, at + 48, at + 64, 0 if st is None else st.data_ptr(), written=written)
         return out, z, st
 
     def backward(self, y, x, params, stats, dout, dz, gate=None, dy=None, dx=None, dgate=None, grads=None):
         """Gradients from those of out and z (either may be None: zero).  Returns (dy, dx, dgate, grads): dgate is None unless gate = "rows";
         grads: dict of float32 [members, width] for the parameters in params (or the tensors given as `grads`, which are overwritten)."""
-        import torch
+        torch = self.torch
         s, work_bytes = self._settings(y, x)
         device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
         if device.type != "cuda":
             raise ValueError("device tensors are wanted")
         if stats.shape != (y.shape[0], 4) or stats.dtype is not torch.float32 or not stats.is_contiguous() or stats.device != device:
             raise ValueError("stats: what forward returned")
+        written = [t for t in (dy, dx, dgate, *(grads or {}).values()) if t is not None]
         if dy is None:
             dy = torch.empty_like(y)
         if dx is None:
@@ -732,5 +752,5 @@ class BlockNorm:
         at = C.addressof(a)
         work = torch.empty(work_bytes, dtype=torch.uint8, device=device)   # (of this call: calls on two streams do not meet in it)
         _call(device, lib().pbt_block_norm_backward, C.byref(s), at, at + 16, at + 32, at + 128, stats.data_ptr(), at + 48, at + 64, at + 80, at + 96, at + 112, at + 176,
-              work.data_ptr(), work_bytes)
+              work.data_ptr(), work_bytes, written=written)
         return dy, dx, dgate, grads

@@ -154,3 +154,51 @@ def test_calls_that_would_lose_a_graph_are_refused():
     param = dict(pre_gain=gain.clone().requires_grad_())
     grads = op.backward(y, h, param, want[2], h, y)[3]
     assert grads["pre_gain"].shape == (1, 16) and not grads["pre_gain"].requires_grad
+
+
+def test_tensors_that_calls_write_are_marked_as_written():
+    """A graph that saved one of them says so in its backward pass instead of using the new values."""
+    rows, d = 6, 16
+    store = torch.ones(1, 4 * d, device="cuda")
+    g = _gen(9)
+
+    def saved(t, write):
+        w = torch.ones_like(t, requires_grad=True)
+        (w * t).sum().backward()             # (untouched: fine)
+        y = (w * t).sum()
+        write()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+
+    x = _normal(g, rows, 2, 8)
+    r = binding.Rotary(8)
+    saved(x, lambda: r(x, start=1))
+    other = _normal(g, rows, 2, 8)
+    saved(other, lambda: r([x, x.clone()], [torch.empty_like(x), other], start=1))
+    grad, bound = _normal(g, 2, 40), torch.full((2,), 1e-3, device="cuda")
+    clip = binding.GradClip([grad, torch.ones(2, d, device="cuda")])
+    saved(grad, lambda: clip(bound))
+    norms = torch.empty(2, device="cuda")
+    saved(norms.zero_(), lambda: clip(norms=norms))
+    columns = binding.GradClip([store[:, :d], store[:, d:2 * d]])
+    saved(store, lambda: columns(bound[:1]))
+    y, h, dout, dz = (_normal(g, rows, d) for _ in range(4))
+    op = binding.BlockNorm(d)
+    stats = op.forward(y, h)[2]
+    dy, dx, gain = torch.zeros_like(y), torch.zeros_like(h), torch.zeros(1, d, device="cuda")
+    params = dict(pre_gain=torch.ones(1, d, device="cuda"))
+    for t in (dy, dx, gain):
+        saved(t, lambda: op.backward(y, h, params, stats, dout, dz, dy=dy, dx=dx, grads=dict(pre_gain=gain)))
+    saved(h, lambda: op.forward(y, h, out=h))
+    saved(y, lambda: op.forward(y, h, z=y))
+    # what is read only stays usable
+    w = torch.ones_like(dout, requires_grad=True)
+    out = (w * dout).sum()
+    op.backward(y, h, {}, stats, dout, dz)
+    clip()
+    out.backward()
+    assert torch.equal(w.grad, dout)
+    with torch.inference_mode():
+        t = torch.ones(3, 1, 8, device="cuda")
+        r(t)
+    r(t)
