@@ -462,7 +462,7 @@ pbt_status pbt_block_norm_backward(const pbt_block_norm* n, const pbt_rows* y, c
                                    const float* d_stats, const pbt_rows* dout, const pbt_rows* dz, const pbt_rows* dy, const pbt_rows* dx,
                                    const pbt_rows* dgate, const pbt_block_params* grads, void* d_work, size_t work_bytes, void* hip_stream);
 
-/* Kernel classes for pbt_timing_enable. */
+/* Kernel classes for pbt_timing_enable.  Launches of other kernels (LayerNorms, dropout, rotary positions, block norms, gradient norms) belong to none. */
 enum {
   PBT_K_NONE = -1,
   PBT_K_FETCH = 0,      /* mini-batch fetch                                  */

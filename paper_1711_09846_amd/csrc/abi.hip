@@ -58,8 +58,8 @@ pbt_status clip_step(pbt_handle* h, OptArgs* oa, hipStream_t s) {
   const Plan& p = h->plan;
   if (p.col_clip < 0) return PBT_OK;
   float* factor = h->sc<float>(p.o_gfactor);
-  PBT_LAUNCH(h, PBT_K_OPTIMIZER, s, grad_factor(h->sc<float>(p.o_grad), p.lay.stride, h->cfg.P, h->st<float>(p.o_hyper) + p.col_clip, h->cfg.n_hyper,
-                                                h->st<float>(p.o_gnorm), factor, h->sc<void>(p.o_gwork), s));
+  PBT_HIP(h, grad_factor(h->sc<float>(p.o_grad), p.lay.stride, h->cfg.P, h->st<float>(p.o_hyper) + p.col_clip, h->cfg.n_hyper, h->st<float>(p.o_gnorm), factor,
+                         h->sc<void>(p.o_gwork), s));
   oa->g_scale = factor;
   return PBT_OK;
 }

@@ -122,7 +122,7 @@ pbt_status turn_heads(const Ctx& x, bf16_t* qkv, int backward) {
   a.period = D.S;   // (rows are whole sequences)
   a.gain = (float)t.opt.rot.gain; a.sign = backward ? -1.f : 1.f;
   a.turns = x.h->st<double>(t.o_turns);
-  PBT_LAUNCH(x.h, PBT_K_HEAD, x.s, rotary_apply(a, t.opt.rot.layout, PBT_DTYPE_BF16, x.s));
+  PBT_HIP(x.h, rotary_apply(a, t.opt.rot.layout, PBT_DTYPE_BF16, x.s));
   return PBT_OK;
 }
 

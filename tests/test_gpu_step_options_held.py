@@ -45,3 +45,23 @@ def test_unused_position_table_under_weight_decay_and_with_moments(clip):
     for j in used:
         part = np.s_[:, lay.seg_off[j]:lay.seg_off[j] + lay.seg_len[j]]
         assert (after[binding.ARR_OPT1][part] != before[binding.ARR_OPT1][part]).any(), j
+
+
+def _launches(wl, H, opt_const=None):
+    pop, pool = _population(wl, H, opt_const)
+    pop.step(pool, 0)
+    classes = (binding.K_HEAD, binding.K_OPTIMIZER)
+    pop.timing_enable_classes(classes, 200)
+    for s in (1, 2):
+        pop.step(pool, s)
+    return [pop.timing_read_class(k)[1] for k in classes]
+
+
+def test_options_launches_are_not_counted_to_other_kernels_classes():
+    """The timed classes hold the same launches with options as without: a class's time over its launches stays that of its kernels."""
+    wl = _reduced(P=2)
+    plain = _launches(wl, H2)
+    assert plain[1] == 2      # one launch of the optimiser a step
+    clip = dict(roles=wl.roles + [W.ROLE_CLIP_NORM], h_max=wl.h_max + [float("inf")], priors=wl.priors + [("log", 0.05, 5.0)])
+    assert _launches(wl.replace(**clip), [h + [0.1] for h in H2]) == plain
+    assert _launches(wl.replace(tf_options=dict(rotary=dict(rot_dim=16), block_norm="rms")), H2) == plain
