@@ -730,7 +730,7 @@ class BlockNorm:
         device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
         if device.type != "cuda":
             raise ValueError("device tensors are wanted")
-        if stats.shape != (y.shape[0], 4) or stats.dtype is not torch.float32 or not stats.is_contiguous() or stats.device != device:
+        if stats is None or stats.shape != (y.shape[0], 4) or stats.dtype is not torch.float32 or not stats.is_contiguous() or stats.device != device:
             raise ValueError("stats: what forward returned")
         written = [t for t in (dy, dx, dgate, *(grads or {}).values()) if t is not None]
         if dy is None:

@@ -202,3 +202,11 @@ def test_tensors_that_calls_write_are_marked_as_written():
         t = torch.ones(3, 1, 8, device="cuda")
         r(t)
     r(t)
+
+
+def test_block_norm_backward_without_statistics_is_refused():
+    y = torch.zeros(2, 16, device="cuda")
+    op = binding.BlockNorm(16)
+    stats = op.forward(y, y, stats=False)[2]
+    with pytest.raises(ValueError, match="stats"):
+        op.backward(y, y, {}, stats, y, y)
