@@ -6,34 +6,9 @@
 // their gradients add up in registers.  The next row is requested as soon as this one's values have been taken over: loads are single instructions without a
 // branch around their results, which the compiler would wait at (with such branches 8191 rows of 5001 took 129 us forward, 94 now).
 #pragma once
-#include <algorithm>
-
 #include "operators.h"
 
 namespace pbt {
-
-constexpr int WIDE = 0;   // T of a team that is the whole workgroup
-struct BlockTeam { int T, threads, rows; };   // threads of a workgroup, rows it has at a time
-inline BlockTeam block_team(int d) {
-  if (d <= 64) return {8, 256, 32};
-  if (d <= 128) return {16, 256, 16};
-  if (d <= 256) return {32, 256, 8};
-  if (d <= 512) return {64, 256, 4};
-  return {WIDE, (d + 511) / 512 * 64, 1};
-}
-
-// Rows of a slab.  What a slab costs besides its rows (`extra` bytes a column: parameters read, sums written and read again) should be an eighth of what
-// its rows move (`moved` bytes a column and row) and a team should see eight rows, while every compute unit has `resident` workgroups, and there
-// are at most `most` in all.
-inline int64_t slab_rows(const pbt_block_norm& n, int extra, int moved, int resident, int most) {
-  const BlockTeam t = block_team(n.d);
-  const int64_t all = n.rows * n.P;
-  int64_t rows = std::max<int64_t>((8 * extra + moved - 1) / moved, 8 * t.rows);
-  rows = std::min(rows, (all + 256 * resident - 1) / (256 * resident));   // (rounded up: a few workgroups more than fit would double the time)
-  rows = std::max(rows, (all + most - 1) / most);
-  rows = (rows + t.rows - 1) / t.rows * t.rows;
-  return std::max<int64_t>(std::min(rows, n.rows), 1);
-}
 
 // over T = 8, 16 or 32 adjacent lanes: quads change places, half rows are mirrored (quads are equal by then), rows of 16 are mirrored, two rows are swapped
 template <int T>
@@ -110,8 +85,7 @@ __device__ __forceinline__ void clear_past(float* v, int n) {
 
 // How a wavefront reads a row's eight elements a lane.  The lane at the row's end reads the eight that end there, its neighbours' among them: those must be
 // of the same wavefront, whose loads come before its stores (another one may have written its part already where an output lies over the input).
-// ALONE: widths whose last wavefront has fewer than eight elements in all, which are read one by one.
-inline bool ends_alone(int d) { return d < 8 || (d > 512 && d % 512 > 0 && d % 512 < 8); }
+// ALONE (block_ends_alone): widths whose last wavefront has fewer than eight elements in all, which are read one by one.
 template <bool ALONE> struct RowReader {
   bool alone;   // this is that wavefront
   int n;

@@ -6,7 +6,6 @@
 // and 128 from LDS, registers are what limits how many rows are on their way.
 // Bound by memory: 16 x 4096 rows of 512 with a gate a row and the stream in fp32, 738 MB: 150 us (4.9 TB/s); 16384 rows of 2048: 131 (4.6); 8191 rows of 5001:
 // 115 (4.3).  The second launch: 4 to 10 us.
-#include <algorithm>
 #include <type_traits>
 
 #include "block_norm.h"
@@ -251,14 +250,7 @@ __global__ __launch_bounds__(256) void block_param_kernel(const float* __restric
   if (grp == 0 && c < d) out[i * g.stride + c] = ((red[0][cl] + red[1][cl]) + red[2][cl]) + red[3][cl];
 }
 
-// (every gradient counted: the working memory does not depend on which are asked for)
-int64_t rows_per_slab(const pbt_block_norm& n) {
-  const int a = n.dtype == PBT_DTYPE_BF16 ? 2 : 4, r = n.res_dtype == PBT_DTYPE_BF16 ? 2 : 4;
-  const int norms = (n.post != PBT_NORM_NONE) + (n.pre != PBT_NORM_NONE), sums = 2 * norms + (n.gate == PBT_GATE_VECTOR);
-  const int moved = (n.pre != PBT_NORM_NONE ? 3 : 2) * a + (n.gate == PBT_GATE_ROWS ? 2 * a : 0) + 3 * r;
-  return slab_rows(n, 4 * sums + 8 * sums, moved, std::max(8 / (block_team(n.d).threads / 64), 1), 2048);
-}
-int64_t slabs_of(const pbt_block_norm& n) { return (n.rows + rows_per_slab(n) - 1) / rows_per_slab(n); }
+int64_t slabs_of(const pbt_block_norm& n) { return (n.rows + block_backward_slab(n) - 1) / block_backward_slab(n); }
 
 // more than 64 KB of LDS need a permission, once on every device (wide teams have 72 to 128 KB, whose compute unit has no room for a second of them anyway)
 template <class A, class R, int MOST, bool ALL, bool ALONE>
@@ -273,10 +265,10 @@ hipError_t launch_wide(const BlockArgs& a, int64_t per_slab, dim3 grid, dim3 blo
 template <class A, class R>
 hipError_t launch(const BlockArgs& a, int64_t slabs, hipStream_t s) {
   const BlockTeam t = block_team(a.n.d);
-  const int64_t per_slab = rows_per_slab(a.n);
+  const int64_t per_slab = block_backward_slab(a.n);
   const dim3 grid((unsigned)slabs, a.n.P), block(t.threads);
   const size_t lds = (size_t)(t.T == WIDE ? PARAMS : SUMS) * 2 * (t.T == WIDE ? t.threads : t.T) * sizeof(float4);
-  if (ends_alone(a.n.d)) {
+  if (block_ends_alone(a.n.d)) {
     if (t.T == WIDE) return launch_wide<A, R, 1024, true, true>(a, per_slab, grid, block, lds, s);
     hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, true, true>), grid, block, lds, s, a, per_slab);
   } else if (t.T == 8) hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, true, false>), grid, block, lds, s, a, per_slab);

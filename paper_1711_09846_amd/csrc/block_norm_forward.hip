@@ -2,7 +2,6 @@
 // Bound by memory: 16 x 4096 rows of 512 bf16 with a gate vector, 268 MB: 53 to 59 us; with a gate a row and the stream in fp32, 470 MB: 88 (5.3 TB/s); 16384 rows of
 // 2048: 84 (4.8).  Rows of ten wavefronts leave two workgroups a compute unit, and three barriers a row show: 8191 rows of 5001: 94 us (3.5 TB/s).  4 rows of
 // 2048: 3.4 us.
-#include <algorithm>
 #include <type_traits>
 
 #include "block_norm.h"
@@ -85,12 +84,11 @@ __global__ __launch_bounds__(MOST) void block_forward_kernel(BlockArgs a, int64_
 template <class A, class R>
 void launch(const BlockArgs& a, hipStream_t s) {
   const BlockTeam t = block_team(a.n.d);
-  int extra = 0;
-  for (const float* p : {a.p.post_gain, a.p.post_bias, a.p.pre_gain, a.p.pre_bias, a.p.gate}) extra += p ? 4 : 0;
-  const int moved = (int)((a.n.pre != PBT_NORM_NONE ? 2 : 1) * sizeof(A) + (a.n.gate == PBT_GATE_ROWS ? sizeof(A) : 0) + 2 * sizeof(R));
-  const int64_t per_slab = slab_rows(a.n, extra, moved, std::max(16 / (t.threads / 64), 1), 4096);
+  int params = 0;
+  for (const float* p : {a.p.post_gain, a.p.post_bias, a.p.pre_gain, a.p.pre_bias, a.p.gate}) params += p ? 1 : 0;
+  const int64_t per_slab = block_forward_slab(a.n, params);
   const dim3 grid((unsigned)((a.n.rows + per_slab - 1) / per_slab), a.n.P), block(t.threads);
-  if (ends_alone(a.n.d)) {
+  if (block_ends_alone(a.n.d)) {
     if (t.T == WIDE) hipLaunchKernelGGL((block_forward_kernel<A, R, WIDE, 1024, true>), grid, block, 0, s, a, per_slab);
     else hipLaunchKernelGGL((block_forward_kernel<A, R, 8, 256, true>), grid, block, 0, s, a, per_slab);
   } else if (t.T == 8) hipLaunchKernelGGL((block_forward_kernel<A, R, 8, 256, false>), grid, block, 0, s, a, per_slab);

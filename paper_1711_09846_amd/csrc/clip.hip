@@ -9,14 +9,11 @@
 // 202 thousand, which the cache holds: 57 to 62 us; 3 members of 6 million bf16 at odd addresses: 26; 8 members of 2372 floats: 3.9.  (Members in batches of half the
 // cache, so that every second read is served by it: 882 us for the first of these, the launches are too short to run at the memory's rate.  Vectors moved to
 // multiples of 16 bytes: 2 to 7 % slower, an access that crosses a line costs less than the tests.)
-#include <algorithm>
-
 #include "operators.h"
 
 namespace pbt {
 namespace {
 
-constexpr int CLIP_TENSORS = 64;   // of one launch (the table is a kernel argument)
 struct ClipTable {
   const char* src[CLIP_TENSORS];
   char* dst[CLIP_TENSORS];
@@ -116,11 +113,10 @@ __device__ __forceinline__ float factor(double n, const float* max_norm) {
 
 // ---- small members: held in registers ----
 // PER units a thread.  (More of them would leave a compute unit one workgroup: 1024 members of 20000 floats take 31 us with 4, 49 with 8.)
-constexpr int HELD_THREADS = 1024;
 template <int PER>
-__global__ __launch_bounds__(HELD_THREADS) void clip_held_kernel(ClipTable table, const float* __restrict__ max_norm, int64_t max_norm_stride, float* __restrict__ norm) {
+__global__ __launch_bounds__(CLIP_HELD_THREADS) void clip_held_kernel(ClipTable table, const float* __restrict__ max_norm, int64_t max_norm_stride, float* __restrict__ norm) {
   __shared__ uint64_t words[TABLE_WORDS];
-  __shared__ double red[HELD_THREADS / 64];
+  __shared__ double red[CLIP_HELD_THREADS / 64];
   const int i = blockIdx.x;
   const Lookup t = copy_table(table, words);
   const int64_t total = t.start(t.n);
@@ -129,7 +125,7 @@ __global__ __launch_bounds__(HELD_THREADS) void clip_held_kernel(ClipTable table
   double s = 0.0;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
-    const int64_t at = threadIdx.x + j * HELD_THREADS;
+    const int64_t at = threadIdx.x + j * CLIP_HELD_THREADS;
     u[j] = Unit8{};
     if (at < total) {
       const Place p = place(t, i, at);
@@ -139,18 +135,18 @@ __global__ __launch_bounds__(HELD_THREADS) void clip_held_kernel(ClipTable table
   }
 #pragma unroll
   for (int j = 0; j < PER; ++j)
-    if (threadIdx.x + j * HELD_THREADS < total) {
+    if (threadIdx.x + j * CLIP_HELD_THREADS < total) {
       float v[8];
       unpack(u[j], (half >> j) & 1, v);
       s = squares(v, s);
     }
-  const double n = sqrt(block_sum<HELD_THREADS>(s, red));
+  const double n = sqrt(block_sum<CLIP_HELD_THREADS>(s, red));
   if (norm && threadIdx.x == 0) norm[i] = (float)n;
   if (!max_norm) return;
   const float c = factor(n, max_norm + i * max_norm_stride);
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
-    const int64_t at = threadIdx.x + j * HELD_THREADS;
+    const int64_t at = threadIdx.x + j * CLIP_HELD_THREADS;
     if (at >= total) break;
     const Place p = place(t, i, at);
     if (c == 1.f && p.src == p.dst) continue;
@@ -286,32 +282,6 @@ __global__ __launch_bounds__(256) void clip_factor_kernel(const double* __restri
   }
 }
 
-int64_t units(const pbt_grad& g) { return (g.len + 7) / 8; }
-int64_t units_of(const pbt_grad* g, int k0, int n) {
-  int64_t total = 0;
-  for (int k = k0; k < n && k < k0 + CLIP_TENSORS; ++k) total += units(g[k]);
-  return total;
-}
-// Units a thread holds where members are held, 0: they are not.  A workgroup a member: up to 4 units a thread whatever the number of members (one of 30000 floats:
-// 5 us, 7 in two launches), 8 where there are members for a quarter of the compute units (128 of 60000 floats: 16 us, 20 in two launches; one: 10.5, 7.0).
-int held(const pbt_grad* g, int n, int P) {
-  if (n > CLIP_TENSORS) return 0;
-  const int64_t u = units_of(g, 0, n);
-  return u <= 4 * HELD_THREADS ? 4 : u <= 8 * HELD_THREADS && P >= 64 ? 8 : 0;
-}
-// ranges of a launch over `total` units of each of P members: at least `least` units each, about `grid` workgroups, at most `most` a member
-int64_t ranges_of(int64_t total, int P, int64_t least, int64_t grid, int64_t most) {
-  return std::max<int64_t>(std::min(std::min((total + least - 1) / least, most), std::max<int64_t>(grid / P, 1)), 1);
-}
-// (Sums: a member's few hundred ranges are added up again by every workgroup of the second launch.  8192 workgroups instead of 2048: 128 x 202k floats 62 us
-// instead of 60.  Factors: 16 x 21M floats take 762 us with 8192 workgroups, 743 with 32768.)
-int64_t sum_ranges(int64_t total, int P) { return ranges_of(total, P, 256, 2048, 1024); }
-int64_t scale_ranges(int64_t total, int P) { return ranges_of(total, P, 1024, 32768, 32768); }
-int64_t parts(const pbt_grad* g, int n, int P) {
-  int64_t sum = 0;
-  for (int k0 = 0; k0 < n; k0 += CLIP_TENSORS) sum += sum_ranges(units_of(g, k0, n), P);
-  return sum;
-}
 ClipTable table(const pbt_grad* g, int k0, int n, bool* in_place) {
   ClipTable t;
   t.n = std::min(n - k0, CLIP_TENSORS);
@@ -324,7 +294,7 @@ ClipTable table(const pbt_grad* g, int k0, int n, bool* in_place) {
     t.dst[k] = static_cast<char*>(e.d_dst);
     t.len[k] = e.len; t.src_stride[k] = e.src_stride; t.dst_stride[k] = e.dst_stride;
     t.start[k] = at;
-    at += units(e);
+    at += clip_units(e);
     if (e.dtype == PBT_DTYPE_BF16) t.bf16 |= 1ull << k;
     if (e.d_src != e.d_dst) *in_place = false;
   }
@@ -339,17 +309,17 @@ ClipTable table(const pbt_grad* g, int k0, int n, bool* in_place) {
 
 }  // namespace
 
-size_t clip_work_bytes(const pbt_grad* g, int n, int P) { return (size_t)P * parts(g, n, P) * sizeof(double); }
+size_t clip_work_bytes(const pbt_grad* g, int n, int P) { return (size_t)P * clip_parts(g, n, P) * sizeof(double); }
 
 size_t grad_factor_work_bytes(int64_t stride, int P) {
   const pbt_grad g{nullptr, nullptr, stride, stride, stride, PBT_DTYPE_FP32, 0};
-  return (size_t)P * parts(&g, 1, P) * sizeof(double);
+  return (size_t)P * clip_parts(&g, 1, P) * sizeof(double);
 }
 hipError_t grad_factor(const float* G, int64_t stride, int P, const float* max_norm, int64_t max_norm_stride, float* norm, float* out, void* work, hipStream_t s) {
   const pbt_grad g{G, nullptr, stride, stride, stride, PBT_DTYPE_FP32, 0};
   bool in_place;
   const ClipTable t = table(&g, 0, 1, &in_place);
-  const int64_t total = t.start[1], ranges = sum_ranges(total, P), per_range = (total + ranges - 1) / ranges;
+  const int64_t total = t.start[1], ranges = clip_sum_ranges(total, P), per_range = (total + ranges - 1) / ranges;
   double* part = static_cast<double*>(work);
   hipLaunchKernelGGL(clip_sum_kernel, dim3((unsigned)ranges, P), dim3(256), 0, s, t, per_range, part, ranges, (int64_t)0);
   hipLaunchKernelGGL(clip_factor_kernel, dim3(P), dim3(256), 0, s, part, ranges, max_norm, max_norm_stride, norm, out);
@@ -358,27 +328,27 @@ hipError_t grad_factor(const float* G, int64_t stride, int P, const float* max_n
 
 hipError_t clip_gradients(const pbt_grad* g, int n, int P, const float* max_norm, int64_t max_norm_stride, float* norm, void* work, hipStream_t s) {
   bool in_place;
-  if (const int per = held(g, n, P)) {
+  if (const int per = clip_held(g, n, P)) {
     const ClipTable t = table(g, 0, n, &in_place);
-    if (per == 4) hipLaunchKernelGGL(clip_held_kernel<4>, dim3(P), dim3(HELD_THREADS), 0, s, t, max_norm, max_norm_stride, norm);
-    else hipLaunchKernelGGL(clip_held_kernel<8>, dim3(P), dim3(HELD_THREADS), 0, s, t, max_norm, max_norm_stride, norm);
+    if (per == 4) hipLaunchKernelGGL(clip_held_kernel<4>, dim3(P), dim3(CLIP_HELD_THREADS), 0, s, t, max_norm, max_norm_stride, norm);
+    else hipLaunchKernelGGL(clip_held_kernel<8>, dim3(P), dim3(CLIP_HELD_THREADS), 0, s, t, max_norm, max_norm_stride, norm);
     return hipGetLastError();
   }
   double* part = static_cast<double*>(work);
-  const int64_t n_part = parts(g, n, P);
+  const int64_t n_part = clip_parts(g, n, P);
   int64_t bytes = 0;
   for (int k = 0; k < n; ++k) bytes += P * g[k].len * (g[k].dtype == PBT_DTYPE_BF16 ? 2 : 4);
   for (int pass = 0; pass < 2; ++pass) {
     int64_t first = 0;
     for (int k0 = 0; k0 < n; k0 += CLIP_TENSORS) {
       const ClipTable t = table(g, k0, n, &in_place);
-      const int64_t total = t.start[t.n], ranges = pass == 0 ? sum_ranges(total, P) : max_norm ? scale_ranges(total, P) : 1, per_range = (total + ranges - 1) / ranges;
+      const int64_t total = t.start[t.n], ranges = pass == 0 ? clip_sum_ranges(total, P) : max_norm ? clip_scale_ranges(total, P) : 1, per_range = (total + ranges - 1) / ranges;
       const dim3 grid((unsigned)ranges, P);
       if (pass == 0)
         hipLaunchKernelGGL(clip_sum_kernel, grid, dim3(256), 0, s, t, per_range, part, n_part, first);
       else if (!max_norm && k0 > 0)
         break;
-      else if (bytes > LAST_CACHE / 4)   // (128 x 202k floats, 104 MB: 63 us so, 72 through the caches; 37 MB: no difference)
+      else if (clip_past_caches(bytes))
         hipLaunchKernelGGL(clip_scale_kernel<true>, grid, dim3(256), 0, s, t, per_range, part, n_part, max_norm, max_norm_stride, k0 == 0 ? norm : nullptr, (int)in_place);
       else
         hipLaunchKernelGGL(clip_scale_kernel<false>, grid, dim3(256), 0, s, t, per_range, part, n_part, max_norm, max_norm_stride, k0 == 0 ? norm : nullptr, (int)in_place);

@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "operators_choose.h"
 #include "../../include/pbt.h"
 
 namespace pbt {
@@ -20,7 +21,6 @@ __device__ __forceinline__ void stream16(void* p, const Vec16& v) {
   const u32x4_any x = {v.w[0], v.w[1], v.w[2], v.w[3]};
   __builtin_nontemporal_store(x, static_cast<u32x4_any*>(p));
 }
-constexpr int64_t LAST_CACHE = (int64_t)256 << 20;   // bytes of the cache in front of memory: what a call writes beyond it is not found there afterwards
 
 // Eight elements as they lie in memory, of which n exist (n >= 8: all; n <= 0: none).  load: one by one where n < 8.  load_end: where at least eight
 // elements end at p + n, the eight that do; get_end moves them to their places, away from the load, which is then one instruction that nothing waits for.

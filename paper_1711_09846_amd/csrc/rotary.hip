@@ -9,7 +9,6 @@
 #include <cmath>
 
 #include "operators.h"
-#include "operators_choose.h"
 
 namespace pbt {
 namespace {
@@ -205,8 +204,7 @@ hipError_t launch(RotaryArgs a, hipStream_t s) {
   const size_t lds = (size_t)cut.table * sizeof(float);
   int64_t bytes = 0;
   for (int g = 0; g < a.n_groups; ++g) bytes += a.rows * a.g[g].heads * a.width * (int64_t)sizeof(T);
-  // (131072 rows, 1.3 GB: 495 us past the caches, 514 through them; 65536 rows, 134 MB: 63 and 58)
-  if (bytes > LAST_CACHE) hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, true>), dim3((unsigned)cut.blocks), dim3(256), lds, s, a, cut.shapes, cut.pitch);
+  if (rotary_past_caches(bytes)) hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, true>), dim3((unsigned)cut.blocks), dim3(256), lds, s, a, cut.shapes, cut.pitch);
   else hipLaunchKernelGGL((rotary_kernel<T, LAYOUT, false>), dim3((unsigned)cut.blocks), dim3(256), lds, s, a, cut.shapes, cut.pitch);
   return hipGetLastError();
 }
