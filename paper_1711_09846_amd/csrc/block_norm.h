@@ -52,17 +52,28 @@ template <> struct TeamSum<WIDE> {
   }
 };
 
-// the gate's factor a(g), and a'(g) (SLOPE)
+// The gate's factor a(g), and a'(g) (SLOPE).  Slopes keep their relative precision where the gate is nearly 1, as differences from 1 would not:
+// 1 - tanh(g)^2 = e^(-2|g|) (1 + |tanh g|)^2, by 4 |g| + 8 half steps (the exponent's rounding), and 1 - sigmoid(g) = e^(-g) sigmoid(g).
 template <bool SLOPE>
 __device__ __forceinline__ void gate8(int act, const float* g, float* f, float* df) {
   switch (act) {
     case PBT_ACT_TANH:
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { f[e] = tanhf(g[e]); if (SLOPE) df[e] = 1.f - f[e] * f[e]; }
+      for (int e = 0; e < 8; ++e) {
+        f[e] = tanhf(g[e]);
+        if (SLOPE) {
+          const float q = 1.f + fabsf(f[e]);
+          df[e] = __builtin_amdgcn_exp2f(-2.88539008f * fabsf(g[e])) * q * q;
+        }
+      }
       break;
     case PBT_ACT_SIGMOID:
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { f[e] = 1.f / (1.f + expf(-g[e])); if (SLOPE) df[e] = f[e] * (1.f - f[e]); }
+      for (int e = 0; e < 8; ++e) {
+        const float t = expf(-g[e]);
+        f[e] = 1.f / (1.f + t);
+        if (SLOPE) df[e] = f[e] > 0.f ? t * f[e] * f[e] : f[e];   // (0 where t is infinite)
+      }
       break;
     case PBT_ACT_SILU:
 #pragma unroll

@@ -5,6 +5,7 @@ import torch
 
 from oracle import operators as oo
 from paper_1711_09846_amd import binding
+from tests.test_gpu_operators import CHAIN, _case, _close, _cpu, _magnitudes
 
 pytestmark = pytest.mark.gpu
 
@@ -210,3 +211,34 @@ def test_block_norm_backward_without_statistics_is_refused():
     stats = op.forward(y, y, stats=False)[2]
     with pytest.raises(ValueError, match="stats"):
         op.backward(y, y, {}, stats, y, y)
+
+
+@pytest.mark.parametrize("act,far", [("tanh", 12.0), ("sigmoid", 22.0), ("silu", 22.0)])
+@pytest.mark.parametrize("gate", ["rows", "vector"])
+def test_block_norm_gradients_of_saturated_gates(gate, act, far):
+    """A gate's slope keeps its relative precision where the gate is nearly 0 or 1 (the float64 oracle's own does as far as is looked at here: 1 - tanh(12)^2 is
+    1.5e-10).  dgate = beta a'(g) u t, the rest of it as in test_gpu_operators.py.  a'(g): by at most 16 U of itself (silu: of s (1 + |g| (1 - s)), its terms); tanh:
+    the exponent 2 |g| log2 e is off by the roundings of its constant and its product, 2 U of itself, which moves the exponential by 4 |g| U of itself."""
+    rows, d = 40, 64
+    kw = dict(post="rms", pre="rms", gate=gate, act=act, dtype="fp32", res="fp32")
+    c = _case(1, rows, d, **kw)
+    g = torch.linspace(-far, far, rows * d if gate == "rows" else d).cuda()
+    if gate == "rows":
+        c["gate"] = g.view(rows, d)
+    else:
+        c["params"]["gate"] = g.view(1, d)
+    op, spec = binding.BlockNorm(d, post="rms", pre="rms", gate=gate, act=act, alpha=0.9, beta=0.7), oo.BlockNorm("rms", "rms", gate, act, alpha=0.9, beta=0.7)
+    _, _, stats = op.forward(c["y"], c["x"], c["params"], gate=c["gate"])
+    _, _, dgate, grads = op.backward(c["y"], c["x"], c["params"], stats, c["dout"], c["dz"], gate=c["gate"])
+    p = {k: _cpu(v[0]) for k, v in c["params"].items()}
+    arrays = [None if c[k] is None else _cpu(c[k]) for k in ("y", "x", "gate", "dout", "dz")]
+    w = spec.backward(spec.forward(arrays[0], arrays[1], p, arrays[2])[2], arrays[3], arrays[4])
+    m = _magnitudes(spec, arrays[0], arrays[1], p, *arrays[2:])
+    got, want, mag = (dgate, w[2], m["dgate"]) if gate == "rows" else (grads["gate"][0], w[3]["gate"], m["gate"])
+    tol = (1.01 * CHAIN + 16 + (rows if gate == "vector" else 0) + (4 * np.abs(_cpu(g)).reshape(mag.shape) if act == "tanh" else 0)) * U * mag
+    if act == "silu":
+        gn = _cpu(g)
+        s = 1.0 / (1.0 + np.exp(-gn))
+        slope = np.abs(s * (1.0 + gn * (1.0 - s)))
+        tol = tol * np.maximum(1.0, s * (1.0 + np.abs(gn) * (1.0 - s)) / np.maximum(slope, 1e-30)).reshape(mag.shape)
+    _close(got, want, tol, act)
