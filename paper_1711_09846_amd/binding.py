@@ -207,6 +207,9 @@ def make_tf_options(wl):
     opts = getattr(wl, "tf_options", None)
     if not opts:
         return None
+    unknown = set(opts) - {"rotary", "learned_positions", "block_norm", "alpha", "beta"}
+    if unknown:
+        raise ValueError("tf_options has no %s" % ", ".join(sorted(unknown)))
     o = PbtTfOptions(0, int(opts.get("learned_positions", True)), _choice(_NORMS, opts.get("block_norm", "none"), "block_norm"),
                      opts.get("alpha", 1.0), opts.get("beta", 1.0), 0)
     if opts.get("rotary"):
