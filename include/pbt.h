@@ -216,8 +216,8 @@ typedef struct {
   double base;                      /* > 0, finite */
   double factor;                    /* > 0, finite (LINEAR, BASE, RAMP) */
   double trained_len, low, high;    /* RAMP: trained_len > 0, low < high */
-  double gain;                      /* finite; multiplies the rotated part */
-} pbt_rotary;
+  double gain;                      /* finite, as a float too; multiplies the rotated part */
+} pbt_rotary;                       /* (base and factor give finite frequencies, BASE a finite base: PBT_EINVAL otherwise) */
 #define PBT_ROTARY_MAX_DIM 512
 enum { PBT_NORM_NONE = 0, PBT_NORM_LAYER = 1, PBT_NORM_RMS = 2 };
 

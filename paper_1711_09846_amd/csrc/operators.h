@@ -107,6 +107,8 @@ struct RotaryFrequencies { double turns[PBT_ROTARY_MAX_DIM / 2]; };
 hipError_t rotary_plan(const RotaryFrequencies& f, int n, double* table, hipStream_t s);
 // turns per position of every pair
 void rotary_frequencies(const pbt_rotary& r, RotaryFrequencies* f);
+// the same, refused where they are not finite (operators_abi.hip; settings that check_rotary lets pass)
+pbt_status check_rotary_frequencies(const pbt_rotary* r, RotaryFrequencies* f);
 struct RotaryArgs {
   pbt_heads g[4];
   int n_groups;

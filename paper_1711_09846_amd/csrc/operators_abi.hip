@@ -19,11 +19,17 @@ pbt_status check_rotary(const pbt_rotary* r) {
   if (r->scaling < PBT_ROTARY_SCALE_NONE || r->scaling > PBT_ROTARY_SCALE_RAMP) return fail(nullptr, PBT_EINVAL, "unknown rotary scaling %d", r->scaling);
   if (r->unused != 0) return fail(nullptr, PBT_EINVAL, "the unused field must be 0");
   if (!(r->base > 0.0) || !std::isfinite(r->base)) return fail(nullptr, PBT_EINVAL, "base must be positive and finite");
-  if (!std::isfinite(r->gain)) return fail(nullptr, PBT_EINVAL, "gain must be finite");
+  if (!std::isfinite((float)r->gain)) return fail(nullptr, PBT_EINVAL, "gain must be finite, as a float too");
   if (r->scaling != PBT_ROTARY_SCALE_NONE && (!(r->factor > 0.0) || !std::isfinite(r->factor))) return fail(nullptr, PBT_EINVAL, "factor must be positive and finite");
   if (r->scaling == PBT_ROTARY_SCALE_RAMP &&
       (!(r->trained_len > 0.0) || !std::isfinite(r->trained_len) || !(r->low < r->high) || !std::isfinite(r->low) || !std::isfinite(r->high)))
     return fail(nullptr, PBT_EINVAL, "ramp scaling needs trained_len > 0 and low < high, finite");
+  return PBT_OK;
+}
+pbt_status check_rotary_frequencies(const pbt_rotary* r, RotaryFrequencies* f) {
+  rotary_frequencies(*r, f);
+  for (int j = 0; j < r->rot_dim / 2; ++j)
+    if (!std::isfinite(f->turns[j])) return fail(nullptr, PBT_EINVAL, "base and factor take the frequency of pair %d out of range", j);
   return PBT_OK;
 }
 }  // namespace pbt
@@ -216,7 +222,7 @@ pbt_status pbt_rotary_plan(const pbt_rotary* r, void* d_table, size_t table_byte
   const int pairs = r->rot_dim / 2;
   if (table_bytes < pairs * sizeof(double)) return fail(nullptr, PBT_ENOMEM, "table: %zu bytes given, %zu needed", table_bytes, pairs * sizeof(double));
   RotaryFrequencies f;
-  rotary_frequencies(*r, &f);
+  TRY(check_rotary_frequencies(r, &f));
   const hipError_t e = rotary_plan(f, pairs, static_cast<double*>(d_table), static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return fail(nullptr, PBT_EDEVICE, "writing the rotary table failed: %s", hipGetErrorString(e));
   return PBT_OK;

@@ -217,7 +217,7 @@ void rotary_frequencies(const pbt_rotary& r, RotaryFrequencies* f) {
   for (int j = 0; j < PBT_ROTARY_MAX_DIM / 2; ++j) {
     f->turns[j] = 0.0;
     if (j >= r.rot_dim / 2) continue;
-    double w = std::pow(base, -2.0 * j / r.rot_dim);   // radians a position
+    double w = std::isfinite(base) ? std::pow(base, -2.0 * j / r.rot_dim) : base;   // radians a position (no base: none)
     if (r.scaling == PBT_ROTARY_SCALE_LINEAR) w /= r.factor;
     if (r.scaling == PBT_ROTARY_SCALE_RAMP) {
       const double at = (r.trained_len * w / two_pi - r.low) / (r.high - r.low), keep = at < 0.0 ? 0.0 : at > 1.0 ? 1.0 : at;

@@ -294,7 +294,9 @@ pbt_status tf_check_options(const pbt_config* c, const pbt_tf_options* o) {
   if (o->block_norm == PBT_NORM_NONE && (o->alpha != 1.f || o->beta != 1.f)) return fail(nullptr, PBT_EINVAL, "alpha and beta other than 1 need a block norm");
   if (o->block_norm != PBT_NORM_NONE && !tf_fused_elementwise(*c)) return fail(nullptr, PBT_EUNSUPPORTED, "block norms are built for d_model up to 2048");
   if (o->rotary) {
-    const pbt_status st = check_rotary(&o->rot);
+    pbt_status st = check_rotary(&o->rot);
+    RotaryFrequencies f;
+    if (st == PBT_OK) st = check_rotary_frequencies(&o->rot, &f);
     if (st != PBT_OK) return st;
     if (c->tf_heads < 1 || o->rot.rot_dim > c->tf_d_model / c->tf_heads) return fail(nullptr, PBT_EINVAL, "rot_dim = %d is more than a head", o->rot.rot_dim);
   }
