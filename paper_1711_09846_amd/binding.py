@@ -462,11 +462,9 @@ def _call(device, fn, *args, written=()):
         mark(written)
 
 
-def _no_graph(tensors):
+def _lost_graph():
     """Results have no graph: where one would be recorded, losing it is refused."""
-    for t in tensors:
-        if t is not None and t.requires_grad:
-            raise ValueError("the results would have no graph, and a tensor of the call requires a gradient: call under torch.no_grad(), or from an autograd.Function")
+    raise ValueError("the results would have no graph, and a tensor of the call requires a gradient: call under torch.no_grad(), or from an autograd.Function")
 
 
 @functools.lru_cache(None)
@@ -592,28 +590,32 @@ class Rotary:
         srcs, dsts = (src, dst) if many else ((src,), (dst,))
         if not srcs or len(srcs) != len(dsts):
             raise ValueError("as many dst as src are wanted, and at least one")
-        if torch.is_grad_enabled():
-            _no_graph((*srcs, *dsts))
         first = srcs[0]
+        if first.dim() != 3:
+            raise ValueError("src and dst: [rows, heads, width] with the same rows and width")
+        (rows, _, width), dtype, index, graph = first.shape, first.dtype, self.device.index, torch.is_grad_enabled()
         groups = (PbtHeads * len(srcs))()
         for g, a, b in zip(groups, srcs, dsts):
-            if a.dim() != 3 or b.shape != a.shape or a.shape[0] != first.shape[0] or a.shape[2] != first.shape[2]:
+            shape = a.shape
+            if len(shape) != 3 or b.shape != shape or shape[0] != rows or shape[2] != width:
                 raise ValueError("src and dst: [rows, heads, width] with the same rows and width")
-            if a.dtype != first.dtype or b.dtype != first.dtype or a.device != self.device or b.device != self.device:
+            if a.dtype != dtype or b.dtype != dtype or a.get_device() != index or b.get_device() != index:
                 raise ValueError("src and dst: one type, on the table's device")
+            if graph and (a.requires_grad or b.requires_grad):
+                _lost_graph()
             sa, sb = a.stride(), b.stride()
-            if a.shape[2] > 1 and (sa[2] != 1 or sb[2] != 1):
+            if width > 1 and (sa[2] != 1 or sb[2] != 1):
                 raise ValueError("a head's elements must be adjacent")
-            g.d_src, g.d_dst, g.heads = a.data_ptr(), b.data_ptr(), a.shape[1]
+            g.d_src, g.d_dst, g.heads = a.data_ptr(), b.data_ptr(), shape[1]
             g.src_row, g.src_head, g.dst_row, g.dst_head = sa[0], sa[1], sb[0], sb[1]
         pos, size = 0, 0
         if positions is not None:
-            if positions.shape != (first.shape[0],) or positions.dtype not in (torch.int32, torch.int64) or not positions.is_contiguous() or positions.device != self.device:
+            if positions.shape != (rows,) or positions.dtype not in (torch.int32, torch.int64) or not positions.is_contiguous() or positions.get_device() != index:
                 raise ValueError("positions: a contiguous int32 or int64 tensor [rows] on the table's device")
             pos, size = positions.data_ptr(), positions.element_size()
-        if _runtime()[1](self.device.index) != self._stream:
+        if _runtime()[1](index) != self._stream:
             self.table.record_stream(torch.cuda.current_stream(self.device))   # (the table's memory is that stream's: not given away before this one is done)
-        _call(self.device, lib().pbt_rotary_apply, C.byref(self.settings), self.table.data_ptr(), groups, len(srcs), _dtype_code(first), first.shape[0], first.shape[2],
+        _call(self.device, lib().pbt_rotary_apply, C.byref(self.settings), self.table.data_ptr(), groups, len(srcs), _dtype_code(first), rows, width,
               pos, size, start, period, int(bool(backward)), written=dsts)
         return dst
 
@@ -658,19 +660,21 @@ class BlockNorm:
         return known
 
     @staticmethod
-    def _rows(t, shape, dtype, device, what):
-        """(address, pitch) of a matrix."""
+    def _rows(t, shape, dtype, index, what, graph=False):
+        """(address, pitch) of a matrix; graph: its graph would be lost."""
         if t is None:
             return 0, 0
-        if t.shape != shape or t.dtype is not dtype or t.device != device:
-            raise ValueError("%s: a tensor %s, %s, on %s is wanted" % (what, tuple(shape), dtype, device))
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+            raise ValueError("%s: a tensor %s, %s, on cuda:%d is wanted" % (what, tuple(shape), dtype, index))
+        if graph and t.requires_grad:
+            _lost_graph()
         pitch, step = t.stride()
         n, d = shape
         if step != 1 and d > 1:
             raise ValueError("%s: a row's elements must be adjacent" % what)
         return t.data_ptr(), pitch if n > 1 else d
 
-    def _params(self, params, device):
+    def _params(self, params, index, graph=False):
         """The fields of pbt_block_params."""
         torch = self.torch
         if not params:
@@ -683,8 +687,10 @@ class BlockNorm:
                 seen += name in params
                 continue
             seen += 1
-            if t.dtype is not torch.float32 or t.device != device or t.shape not in self._param_shapes:
+            if t.dtype is not torch.float32 or t.get_device() != index or t.shape not in self._param_shapes:
                 raise ValueError("%s: float32 [members, width] on the tensors' device" % name)
+            if graph and t.requires_grad:
+                _lost_graph()
             steps = t.stride()
             if steps[-1] != 1 and self.width > 1:
                 raise ValueError("%s: adjacent channels are wanted" % name)
@@ -702,15 +708,13 @@ class BlockNorm:
         """Returns (out, z, stats); z is None with pre = "none", stats (float32 [rows, 4], for backward) with stats = False.  They have no graph
         (`backward` has the gradients): a call on tensors that require one is refused unless gradients are off (torch.no_grad(), the inside of an autograd.Function)."""
         torch = self.torch
-        if torch.is_grad_enabled():
-            _no_graph((y, x, gate, out, z, *params.values()) if params else (y, x, gate, out, z))
         s, _ = self._settings(y, x)
-        device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
+        device, shape, ty, tx, graph = y.device, y.shape, y.dtype, x.dtype, torch.is_grad_enabled()
         if device.type != "cuda":
             raise ValueError("device tensors are wanted")
         if gate is not None and not self._rows_gate:
             raise ValueError("a gate's matrix goes with gate = \"rows\"")
-        written = [t for t in (out, z) if t is not None]
+        written = () if out is None and z is None else [t for t in (out, z) if t is not None]
         if out is None:
             out = torch.empty_like(x)
         if not self._pre:
@@ -719,8 +723,9 @@ class BlockNorm:
             z = torch.empty_like(y)
         st = torch.empty((shape[0], 4), dtype=torch.float32, device=device) if stats else None
         rows = self._rows
-        a = _I64x16(*rows(y, shape, ty, device, "y"), *rows(x, shape, tx, device, "x"), *rows(gate, shape, ty, device, "gate"),
-                    *rows(out, shape, tx, device, "out"), *rows(z, shape, ty, device, "z"), *self._params(params, device))
+        index = device.index
+        a = _I64x16(*rows(y, shape, ty, index, "y", graph), *rows(x, shape, tx, index, "x", graph), *rows(gate, shape, ty, index, "gate", graph),
+                    *rows(out, shape, tx, index, "out", graph), *rows(z, shape, ty, index, "z", graph), *self._params(params, index, graph))
         at = C.addressof(a)
         _call(device, lib().pbt_block_norm_forward, C.byref(s), at, at + 16, at + 32, at + 80, at + 48, at + 64, 0 if st is None else st.data_ptr(), written=written)
         return out, z, st
@@ -733,9 +738,9 @@ class BlockNorm:
         device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
         if device.type != "cuda":
             raise ValueError("device tensors are wanted")
-        if stats is None or stats.shape != (y.shape[0], 4) or stats.dtype is not torch.float32 or not stats.is_contiguous() or stats.device != device:
+        if stats is None or stats.shape != (shape[0], 4) or stats.dtype is not torch.float32 or not stats.is_contiguous() or stats.device != device:
             raise ValueError("stats: what forward returned")
-        written = [t for t in (dy, dx, dgate, *(grads or {}).values()) if t is not None]
+        written = () if dy is None and dx is None and dgate is None and grads is None else [t for t in (dy, dx, dgate, *(grads or {}).values()) if t is not None]
         if dy is None:
             dy = torch.empty_like(y)
         if dx is None:
@@ -749,9 +754,10 @@ class BlockNorm:
             names = [k for k, t in (params or {}).items() if t is not None]
             grads = dict(zip(names, torch.empty((len(names), self.members, self.width), dtype=torch.float32, device=device).unbind(0)))
         rows = self._rows
-        a = _I64x28(*rows(y, shape, ty, device, "y"), *rows(x, shape, tx, device, "x"), *rows(gate, shape, ty, device, "gate"), *rows(dout, shape, tx, device, "dout"),
-                    *rows(dz if self._pre else None, shape, ty, device, "dz"), *rows(dy, shape, ty, device, "dy"), *rows(dx, shape, tx, device, "dx"),
-                    *rows(dgate, shape, ty, device, "dgate"), *self._params(params, device), *self._params(grads, device))
+        index = device.index
+        a = _I64x28(*rows(y, shape, ty, index, "y"), *rows(x, shape, tx, index, "x"), *rows(gate, shape, ty, index, "gate"), *rows(dout, shape, tx, index, "dout"),
+                    *rows(dz if self._pre else None, shape, ty, index, "dz"), *rows(dy, shape, ty, index, "dy"), *rows(dx, shape, tx, index, "dx"),
+                    *rows(dgate, shape, ty, index, "dgate"), *self._params(params, index), *self._params(grads, index))
         at = C.addressof(a)
         work = torch.empty(work_bytes, dtype=torch.uint8, device=device)   # (of this call: calls on two streams do not meet in it)
         _call(device, lib().pbt_block_norm_backward, C.byref(s), at, at + 16, at + 32, at + 128, stats.data_ptr(), at + 48, at + 64, at + 80, at + 96, at + 112, at + 176,

@@ -82,12 +82,17 @@ pbt_status check_grads(const pbt_grad* g, int n, int P, bool clip) {
 // What a call writes is apart from everything else that it touches (a tensor's own src and dst have been looked at).  max_norm NULL: norms only, no dst is written.
 pbt_status check_grads_apart(const pbt_grad* g, int n, int P, const float* max_norm, int64_t max_norm_stride, float* norm, void* work, size_t work_bytes) {
   constexpr int FEW = 128;
-  Region few[FEW];
+  Region few[FEW], *r = few;
+  RegionKey few_keys[FEW], *keys = few_keys;
   std::unique_ptr<Region[]> many;
-  Region* r = few;
-  if (2 * (int64_t)n + 3 > FEW) {
-    many.reset(new (std::nothrow) Region[2 * (size_t)n + 3]);
-    if (!(r = many.get())) return fail(nullptr, PBT_ENOMEM, "out of host memory");
+  std::unique_ptr<RegionKey[]> many_keys;
+  const size_t most = 2 * (size_t)n + 3;
+  if (most > FEW) {
+    many.reset(new (std::nothrow) Region[most]);
+    many_keys.reset(new (std::nothrow) RegionKey[most]);
+    r = many.get();
+    keys = many_keys.get();
+    if (!r || !keys) return fail(nullptr, PBT_ENOMEM, "out of host memory");
   }
   enum { NORM = -1, MAX_NORM = -2, WORK = -3 };
   int m = 0;
@@ -101,7 +106,7 @@ pbt_status check_grads_apart(const pbt_grad* g, int n, int P, const float* max_n
   if (norm) r[m++] = Region{reinterpret_cast<uintptr_t>(norm), (int64_t)P * 4, 0, 1, true, NORM};
   r[m++] = Region{reinterpret_cast<uintptr_t>(work), (int64_t)work_bytes, 0, 1, true, WORK};
   int x, y;
-  if (!find_meeting(r, m, &x, &y)) return PBT_OK;
+  if (!find_meeting(r, keys, m, &x, &y)) return PBT_OK;
   if (x > y) std::swap(x, y);
   if (x >= 0) return fail(nullptr, PBT_EINVAL, "dst of one of the tensors %d and %d overlaps the other", x, y);
   const char* const names[3] = {"norm", "max_norm", "the working memory"};
@@ -180,8 +185,9 @@ struct BlockMemory {
     for (int k = 0; k < 5; ++k) add(q[k], (int64_t)n->d * 4, p->stride * 4, n->P, written, name[k]);
   }
   pbt_status check() {
+    RegionKey keys[24];
     int x, y;
-    if (!find_meeting(r, count, &x, &y)) return PBT_OK;
+    if (!find_meeting(r, keys, count, &x, &y)) return PBT_OK;
     return fail(nullptr, PBT_EINVAL, "%s overlaps %s", names[x], names[y]);
   }
 };

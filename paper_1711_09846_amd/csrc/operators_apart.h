@@ -11,7 +11,6 @@ struct Region {
   int64_t bytes, stride, count;
   bool written;
   int what;
-  int64_t place = 0;   // (find_meeting's own)
 };
 inline int64_t region_span(const Region& r) { return r.bytes <= 0 || r.count <= 0 ? 0 : (r.count - 1) * r.stride + r.bytes; }
 
@@ -40,46 +39,62 @@ inline bool regions_apart(const Region& a, const Region& b) {
   return true;
 }
 
-// The first pair of regions found that meet, one of them written, to *x and *y; false: there is none.  `r` is put in order of addresses.  Regions whose spans
+// A place of its own for every region: what is put in order instead of the regions.
+struct RegionKey {
+  uint64_t at;
+  int region;
+};
+inline void in_order(RegionKey* k, int n) {
+  const auto before = [](const RegionKey& a, const RegionKey& b) { return a.at < b.at; };
+  if (!std::is_sorted(k, k + n, before)) std::sort(k, k + n, before);
+}
+
+// The first pair of regions found that meet, one of them written, to *x and *y; false: there is none.  `key`: room for n.  Regions whose spans
 // meet are looked at together: where all are rows of one stride (a flat array's columns) by their places in a row, else pair by pair.
-inline bool find_meeting(Region* r, int n, int* x, int* y) {
-  const auto by_address = [](const Region& a, const Region& b) { return a.at < b.at; };
-  if (!std::is_sorted(r, r + n, by_address)) std::sort(r, r + n, by_address);
+inline bool find_meeting(const Region* r, RegionKey* key, int n, int* x, int* y) {
+  for (int k = 0; k < n; ++k) key[k] = RegionKey{r[k].at, k};
+  in_order(key, n);
   for (int lo = 0; lo < n;) {
-    uintptr_t end = r[lo].at + (uintptr_t)region_span(r[lo]);
-    bool rows = r[lo].count > 1;
+    const Region& first = r[key[lo].region];
+    uint64_t end = first.at + (uint64_t)region_span(first);
     int hi = lo + 1;
-    for (; hi < n && r[hi].at < end; ++hi) {
-      end = std::max(end, r[hi].at + (uintptr_t)region_span(r[hi]));
-      rows = rows && r[hi].count > 1 && r[hi].stride == r[lo].stride;
+    bool rows = first.count > 1 && first.stride > 0;
+    for (; hi < n && key[hi].at < end; ++hi) {
+      const Region& next = r[key[hi].region];
+      end = std::max(end, next.at + (uint64_t)region_span(next));
+      rows = rows && next.count > 1 && next.stride == first.stride;
     }
     if (hi - lo > 1) {
       bool clear = false;
       if (rows && hi - lo > 8) {
         // places in a row, twice around: what starts before the end of an earlier one meets it (or would, if their spans did: pairs decide then)
-        const uintptr_t base = r[lo].at;
-        const int64_t p = r[lo].stride;
-        const auto by_place = [](const Region& a, const Region& b) { return a.place < b.place; };
-        for (int k = lo; k < hi; ++k) r[k].place = (int64_t)(r[k].at - base) < p ? (int64_t)(r[k].at - base) : (int64_t)(r[k].at - base) % p;
-        if (!std::is_sorted(r + lo, r + hi, by_place)) std::sort(r + lo, r + hi, by_place);
+        const uint64_t p = (uint64_t)first.stride, base = first.at;
+        for (int k = lo; k < hi; ++k) {
+          const uint64_t from = key[k].at - base;
+          key[k].at = from < p ? from : from % p;
+        }
+        in_order(key + lo, hi - lo);
         clear = true;
-        int64_t read = 0, wrote = 0;   // ends of what came before
+        uint64_t read = 0, wrote = 0;   // ends of what came before
         for (int lap = 0; lap < 2 && clear; ++lap)
           for (int k = lo; k < hi && clear; ++k) {
-            if (region_span(r[k]) == 0) continue;
-            const int64_t at = r[k].place + lap * p;
-            clear = at >= wrote && (!r[k].written || at >= read);
-            int64_t& e = r[k].written ? wrote : read;
-            e = std::max(e, at + r[k].bytes);
+            const Region& it = r[key[k].region];
+            if (region_span(it) == 0) continue;
+            const uint64_t at = key[k].at + (lap ? p : 0);
+            clear = at >= wrote && (!it.written || at >= read);
+            uint64_t& e = it.written ? wrote : read;
+            e = std::max(e, at + (uint64_t)it.bytes);
           }
       }
       for (int i = lo; i < hi && !clear; ++i)
-        for (int j = i + 1; j < hi; ++j)
-          if ((r[i].written || r[j].written) && !regions_apart(r[i], r[j])) {
-            *x = r[i].what;
-            *y = r[j].what;
+        for (int j = i + 1; j < hi; ++j) {
+          const Region &a = r[key[i].region], &b = r[key[j].region];
+          if ((a.written || b.written) && !regions_apart(a, b)) {
+            *x = a.what;
+            *y = b.what;
             return true;
           }
+        }
     }
     lo = hi;
   }

@@ -12,8 +12,10 @@ _SOURCE = r"""
 extern "C" int meeting(const long long* fields, int n, int* out) {
   pbt::Region* r = new pbt::Region[n];
   for (int k = 0; k < n; ++k) r[k] = pbt::Region{(uintptr_t)fields[5 * k], fields[5 * k + 1], fields[5 * k + 2], fields[5 * k + 3], fields[5 * k + 4] != 0, k};
-  const bool found = pbt::find_meeting(r, n, out, out + 1);
+  pbt::RegionKey* keys = new pbt::RegionKey[n];
+  const bool found = pbt::find_meeting(r, keys, n, out, out + 1);
   delete[] r;
+  delete[] keys;
   return found;
 }
 // fields: address, row, head, rows, heads, width of both
