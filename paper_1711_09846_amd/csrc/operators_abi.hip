@@ -81,7 +81,7 @@ pbt_status check_grads(const pbt_grad* g, int n, int P, bool clip) {
 
 // What a call writes is apart from everything else that it touches (a tensor's own src and dst have been looked at).  max_norm NULL: norms only, no dst is written.
 pbt_status check_grads_apart(const pbt_grad* g, int n, int P, const float* max_norm, int64_t max_norm_stride, float* norm, void* work, size_t work_bytes) {
-  constexpr int FEW = 128;
+  constexpr int FEW = 256;
   Region few[FEW], *r = few;
   RegionKey few_keys[FEW], *keys = few_keys;
   std::unique_ptr<Region[]> many;
