@@ -419,7 +419,7 @@ typedef struct {
   int32_t heads;
   int32_t unused;                   /* 0 */
 } pbt_heads;
-/* Turns h_groups[0 .. n_groups) (1 to 4: query and key heads of one call share their angles) of `rows` rows and `width` elements a
+/* Turns h_groups[0 .. n_groups) (1 to 4, query and key heads for instance, at the same positions) of `rows` rows and `width` elements a
  * head.  Position of row r: d_positions[r] (int32 or int64 by position_bytes 4 or 8), or with d_positions = NULL
  * start + (period > 0 ? r % period : r).  backward = 1 applies the transposed rotation (the same gain, the angle
  * negated): the gradient of the input from that of the output.  rows = 0 is allowed.  Positions and table are apart from every dst (PBT_EINVAL). */
@@ -433,7 +433,8 @@ pbt_status pbt_rotary_apply(const pbt_rotary* r, const void* d_table, const pbt_
  * N_LAYER(v) = (v - mean v) / sqrt(var v + eps) * gain + bias, N_RMS(v) = v / sqrt(mean v^2 + eps) * gain + bias, N_NONE(v) = v; at most one of the two is
  * NONE.  gate: NONE (factor 1), VECTOR (one of the parameters: a factor per channel, the same for all rows of a member) or ROWS (a matrix); a is
  * gate_act, PBT_ACT_NONE, SIGMOID, SILU or TANH.  y, z, the gate's matrix and their gradients are of `dtype`, x, out and theirs
- * of `res_dtype`; parameters and their gradients are float.  z is formed from out before it is rounded. */
+ * of `res_dtype`; parameters and their gradients are float.  z is formed from out before it is rounded.  A row's
+ * squares are summed in float: rows whose mean square (of y, or of its differences from the mean; of out) leaves float's range lose their spread. */
 enum { PBT_GATE_NONE = 0, PBT_GATE_VECTOR = 1, PBT_GATE_ROWS = 2 };
 #define PBT_BLOCK_NORM_MAX_D 8192
 typedef struct {

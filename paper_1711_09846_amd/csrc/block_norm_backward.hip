@@ -5,7 +5,7 @@
 // slabs' sums go to `part`, and a second launch adds them in slab order.  The parameters wait in LDS: a compute unit gets some eight bytes a cycle from memory
 // and 128 from LDS, registers are what limits how many rows are on their way.
 // Bound by memory: 16 x 4096 rows of 512 with a gate a row and the stream in fp32, 738 MB: 150 us (4.9 TB/s); 16384 rows of 2048: 131 (4.6); 8191 rows of 5001:
-// 115 (4.3).  The second launch: 4 to 10 us.
+// 118 (4.2).  33.5 million elements in rows of 64 take 127 us, of 32 154, of 16 243, of 8 384.  The second launch: 4 to 10 us.
 #include <type_traits>
 
 #include "block_norm.h"
@@ -268,6 +268,8 @@ hipError_t launch(const BlockArgs& a, int64_t slabs, hipStream_t s) {
   const int64_t per_slab = block_backward_slab(a.n);
   const dim3 grid((unsigned)slabs, a.n.P), block(t.threads);
   const size_t lds = (size_t)(t.T == WIDE ? PARAMS : SUMS) * 2 * (t.T == WIDE ? t.threads : t.T) * sizeof(float4);
+  // (Widths that end alone have one instance, for every size of a workgroup and all sums, whose registers spill.  16352 rows of 513: 138 us, 16130 of 520 60;
+  // 8184 of 1025 114, 8128 of 1032 48; 4094 of 2049 90, 4080 of 2056 45.)
   if (block_ends_alone(a.n.d)) {
     if (t.T == WIDE) return launch_wide<A, R, 1024, true, true>(a, per_slab, grid, block, lds, s);
     hipLaunchKernelGGL((block_backward_kernel<A, R, 8, 256, true, true>), grid, block, lds, s, a, per_slab);

@@ -1,6 +1,7 @@
 // Block norms, forward: u = N_post(y), out = alpha x + beta a(gate) u, z = N_pre(out) in one pass over y, x and the gate.
 // Bound by memory: 16 x 4096 rows of 512 bf16 with a gate vector, 268 MB: 53 to 59 us; with a gate a row and the stream in fp32, 470 MB: 88 (5.3 TB/s); 16384 rows of
-// 2048: 84 (4.8).  Rows of ten wavefronts leave two workgroups a compute unit, and three barriers a row show: 8191 rows of 5001: 94 us (3.5 TB/s).  4 rows of
+// 2048: 84 (4.8).  Rows of thousands of elements cost what their addresses do: 8191 rows of 5120, which begin at whole lines of memory, take 70 us (4.8 TB/s), of 5000 81,
+// of 5001 88 (3.7).  Narrow rows leave lanes idle, a team has at least eight: 33.5 million elements in rows of 64 take 45 us, of 32 66, of 16 116, of 8 207.  4 rows of
 // 2048: 3.4 us.
 #include <type_traits>
 

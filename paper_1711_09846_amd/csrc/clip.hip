@@ -6,7 +6,7 @@
 //   Larger ones: the units are cut into equal ranges, a workgroup each.  One launch leaves every range's sum; in the next every workgroup adds up its
 //   member's sums (the same order everywhere) and scales its range, the ranges that were summed last first: what the cache in front of memory still holds.
 // 16 members of 21 million floats (1.34 GB each way): 749 us, three times the gradient at 5.4 TB/s, where a copy, twice the gradient, reaches 5.0; 128 members of
-// 202 thousand, which the cache holds: 57 to 62 us; 3 members of 6 million bf16 at odd addresses: 26; 8 members of 2372 floats: 3.9.  (Members in batches of half the
+// 202 thousand, which the cache holds: 56 us; 3 members of 6 million bf16 at odd addresses: 26; 8 members of 2372 floats: 3.9 to 4.5.  (Members in batches of half the
 // cache, so that every second read is served by it: 882 us for the first of these, the launches are too short to run at the memory's rate.  Vectors moved to
 // multiples of 16 bytes: 2 to 7 % slower, an access that crosses a line costs less than the tests.)
 #include "operators.h"

@@ -1,4 +1,4 @@
-// Launchers behind the operators of include/pbt.h that need no handle (clip.hip, rotary.hip, block_norm.hip), and what their kernels share: groups of
+// Launchers behind the operators of include/pbt.h that need no handle (clip.hip, rotary.hip, block_norm_forward.hip, block_norm_backward.hip), and what their kernels share: groups of
 // eight elements of either type at any address.  Every launcher only enqueues on `s`; arguments have been checked by the entry points.
 #pragma once
 #include <type_traits>
@@ -122,7 +122,7 @@ struct RotaryArgs {
 };
 hipError_t rotary_apply(const RotaryArgs& a, int layout, int dtype, hipStream_t s);
 
-// ---- block_norm.hip ----
+// ---- block_norm_forward.hip, block_norm_backward.hip ----
 struct BlockArgs {
   pbt_block_norm n;
   pbt_block_params p, g;    // parameters, their gradients

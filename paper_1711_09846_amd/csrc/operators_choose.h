@@ -111,7 +111,7 @@ inline RotaryCut rotary_cut(const RotaryCall& a) {
   cut.table = 2 * most_rows * pitch;
   return cut;
 }
-// (131072 rows, 1.3 GB: 495 us past the caches, 514 through them; 65536 rows, 134 MB: 63 and 58)
+// (Passes replayed from a graph: 131072 rows, 1.3 GB: 494 us past the caches, 513 through them; 65536 rows, 134 MB: 63 and 58.)
 inline bool rotary_past_caches(int64_t bytes) { return bytes > LAST_CACHE; }
 
 // ---- block_norm_forward.hip, block_norm_backward.hip ----

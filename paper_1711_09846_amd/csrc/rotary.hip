@@ -4,8 +4,9 @@
 // much as moving a pair takes at the memory's rate, so a workgroup forms them once for a few rows, in LDS, and all heads of those rows use them.  A unit of
 // work is one 16-byte access of adjacent pairs (two where a pair's halves lie apart), one a thread and sweep: with four on their way in a thread's registers
 // fewer workgroups fit a compute unit (131072 rows: 812 us).
-// 16 of 24 heads of 64 in 65536 rows, bf16: 58 us, a copy of the same heads 49; 40 of 60 heads of 128 in 131072 rows: 495 us (5.4 TB/s), a copy 472; fp32 rows
-// of 5 heads of 84 with 42 turned, 9973 of them: 9.7 us, a copy 6.8; 16 rows: 3.1.
+// 16 of 24 heads of 64 in 65536 rows, bf16: 53 us, a copy of the same heads 49; 40 of 60 heads of 128 in 131072 rows: 491 us (5.5 TB/s), a copy 472; fp32 rows
+// of 5 heads of 84 with 42 turned, 9973 of them: 9.5 us, a copy 6.8; 16 rows: 3.0.  A group of heads forms its own angles: 32 heads of 128 in 16384 rows take 41 us
+// in place, one key head in the same call 5 us more (by its bytes 1.3); 50000 rows of one head of 128: 13 us (1.9 TB/s).
 #include <cmath>
 
 #include "operators.h"
