@@ -99,8 +99,8 @@ pbt_status check_grads_apart(const pbt_grad* g, int n, int P, const float* max_n
   for (int k = 0; k < n; ++k) {
     if (g[k].len == 0) continue;
     const int64_t e = (int64_t)elem_bytes(g[k].dtype);
-    if (max_norm) r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_dst), g[k].len * e, g[k].dst_stride * e, P, true, k};
-    if (!max_norm || g[k].d_src != g[k].d_dst) r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_src), g[k].len * e, g[k].src_stride * e, P, false, k};
+    if (max_norm) r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_dst), g[k].len * e, P > 1 ? g[k].dst_stride * e : 0, P, true, k};
+    if (!max_norm || g[k].d_src != g[k].d_dst) r[m++] = Region{reinterpret_cast<uintptr_t>(g[k].d_src), g[k].len * e, P > 1 ? g[k].src_stride * e : 0, P, false, k};
   }
   if (max_norm) r[m++] = Region{reinterpret_cast<uintptr_t>(max_norm), 4, max_norm_stride * 4, max_norm_stride > 0 ? P : 1, false, MAX_NORM};
   if (norm) r[m++] = Region{reinterpret_cast<uintptr_t>(norm), (int64_t)P * 4, 0, 1, true, NORM};
@@ -180,9 +180,10 @@ struct BlockMemory {
     if (m && m->d == out.d && m->pitch == out.pitch) return;
     add_rows(m, type, false, name);
   }
+  // (one member's stride is not looked at, and may be anything)
   void add_params(const pbt_block_params* p, bool written, const char* const* name) {
     float* const* q = &p->post_gain;
-    for (int k = 0; k < 5; ++k) add(q[k], (int64_t)n->d * 4, p->stride * 4, n->P, written, name[k]);
+    for (int k = 0; k < 5; ++k) add(q[k], (int64_t)n->d * 4, n->P > 1 ? p->stride * 4 : 0, n->P, written, name[k]);
   }
   pbt_status check() {
     RegionKey keys[24];
