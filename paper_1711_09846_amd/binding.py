@@ -437,6 +437,12 @@ BLOCK_PARAMS = ("post_gain", "post_bias", "pre_gain", "pre_bias", "gate")
 
 
 @functools.lru_cache(None)
+def _torch():
+    import torch
+    return torch
+
+
+@functools.lru_cache(None)
 def _runtime():
     """(the current device's index, device index -> handle of its current stream, marks tensors as written for autograd's version check): functions, without
     the Python around them where torch offers that (a small call takes 8 us in all)."""
@@ -507,8 +513,7 @@ class GradClip:
     either, whether or not the tensors require a gradient."""
 
     def __init__(self, grads, outs=None):
-        import torch
-        self.torch = torch
+        torch = _torch()
         grads = list(grads)
         outs = grads if outs is None else list(outs)
         if not grads or len(outs) != len(grads):
@@ -536,7 +541,7 @@ class GradClip:
         self._work_bytes = n.value
 
     def __call__(self, max_norm=None, norms=None):
-        torch = self.torch
+        torch = _torch()
         written = () if max_norm is None else self._written
         if norms is None:
             norms = torch.empty(self.P, dtype=torch.float32, device=self.device)
@@ -566,8 +571,7 @@ class Rotary:
     waits for it, so that it can be used on any stream afterwards; a captured graph reads the table when it is replayed and keeps nothing alive."""
 
     def __init__(self, rot_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained=0.0, low=1.0, high=32.0, gain=1.0, device="cuda:0"):
-        import torch
-        self.torch = torch
+        torch = _torch()
         self.settings = rotary_settings(rot_dim, base, layout, scaling, factor, trained, low, high, gain)
         self.device = torch.device(device)
         if self.device.index is None:
@@ -578,12 +582,15 @@ class Rotary:
         stream.synchronize()
         self._stream = stream.cuda_stream
 
+    def __getstate__(self):
+        return dict(self.__dict__, _stream=None)     # (a copy's table belongs to the stream that it is made on)
+
     def __call__(self, src, dst=None, positions=None, start=0, period=0, backward=False):
         """src: tensor [rows, heads, width] with adjacent elements, or up to four of them (query and key heads); dst: the same, None: in place.
         positions: int32 or int64 tensor [rows]; without them row r is at start + (r % period if period else r).  backward: the transposed
         rotation, for gradients.  Returns dst, which has no graph: a call on tensors that require a gradient is refused unless gradients are off
         (torch.no_grad(), the inside of an autograd.Function)."""
-        torch = self.torch
+        torch = _torch()
         if dst is None:
             dst = src
         many = isinstance(src, (list, tuple))
@@ -627,8 +634,7 @@ class BlockNorm:
     with the same distance between members."""
 
     def __init__(self, width, members=1, post="layer", pre="layer", gate="none", act="none", eps=1e-5, alpha=1.0, beta=1.0):
-        import torch
-        self.torch = torch
+        torch = _torch()
         self.width, self.members = width, members
         self.settings = PbtBlockNorm(0, members, width, _choice(_NORMS, post, "post"), _choice(_NORMS, pre, "pre"), _choice(_GATES, gate, "gate"),
                                      _choice(_GATE_ACTS, act, "act"), 0, 0, eps, alpha, beta)
@@ -676,7 +682,7 @@ class BlockNorm:
 
     def _params(self, params, index, graph=False):
         """The fields of pbt_block_params."""
-        torch = self.torch
+        torch = _torch()
         if not params:
             return 0, 0, 0, 0, 0, self.width
         out, stride, seen = [], None, 0
@@ -707,7 +713,7 @@ class BlockNorm:
     def forward(self, y, x, params=None, gate=None, out=None, z=None, stats=True):
         """Returns (out, z, stats); z is None with pre = "none", stats (float32 [rows, 4], for backward) with stats = False.  They have no graph
         (`backward` has the gradients): a call on tensors that require one is refused unless gradients are off (torch.no_grad(), the inside of an autograd.Function)."""
-        torch = self.torch
+        torch = _torch()
         s, _ = self._settings(y, x)
         device, shape, ty, tx, graph = y.device, y.shape, y.dtype, x.dtype, torch.is_grad_enabled()
         if device.type != "cuda":
@@ -733,7 +739,7 @@ class BlockNorm:
     def backward(self, y, x, params, stats, dout, dz, gate=None, dy=None, dx=None, dgate=None, grads=None):
         """Gradients from those of out and z (either may be None: zero).  Returns (dy, dx, dgate, grads): dgate is None unless gate = "rows";
         grads: dict of float32 [members, width] for the parameters in params (or the tensors given as `grads`, which are overwritten)."""
-        torch = self.torch
+        torch = _torch()
         s, work_bytes = self._settings(y, x)
         device, shape, ty, tx = y.device, y.shape, y.dtype, x.dtype
         if device.type != "cuda":

@@ -1,4 +1,7 @@
 """Calls of the operators that their documentation allows, on streams, on memory that is shared or laid out otherwise, and those that are refused."""
+import copy
+import pickle
+
 import numpy as np
 import pytest
 import torch
@@ -242,3 +245,20 @@ def test_block_norm_gradients_of_saturated_gates(gate, act, far):
         slope = np.abs(s * (1.0 + gn * (1.0 - s)))
         tol = tol * np.maximum(1.0, s * (1.0 + np.abs(gn) * (1.0 - s)) / np.maximum(slope, 1e-30)).reshape(mag.shape)
     _close(got, want, tol, act)
+
+
+@pytest.mark.parametrize("how", [copy.deepcopy, lambda o: pickle.loads(pickle.dumps(o))], ids=["deepcopy", "pickle"])
+def test_copies_of_plans(how):
+    """Rotary and BlockNorm hold settings and a table: a copy of a model that has them works like the model."""
+    x = _normal(_gen(3), 6, 2, 32)
+    r, op = binding.Rotary(32, base=500.0), binding.BlockNorm(64, post="rms", pre="rms")
+    y = x.view(6, 64)
+    want = r(x, torch.empty_like(x), start=2), op.forward(y, y)[1]
+    r2, op2 = how(r), how(op)
+    assert r2.table.data_ptr() != r.table.data_ptr()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = r2(x, torch.empty_like(x), start=2), op2.forward(y, y)[1]
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
